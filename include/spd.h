@@ -349,6 +349,117 @@ int spd_build_schedule(const spd_shape *shape, int32_t n_users, const int32_t *l
                        int32_t head_per_wave, spd_work_item *items, int64_t capacity, int64_t *n_items,
                        int32_t *chunk_tokens);
 
+/* ------------------------------------------------------------------------------------------------------------
+ * Several new tokens per user: a prompt, a chunk of one, tokens proposed for checking, or one token each with scores
+ * that are more than scaled products.  What is written into a cache (rotated keys, values) and the partial attention
+ * that reads it.  Token arrays hold the users' new tokens one user after the other, n_new[u] of user u (ragged;
+ * T = sum of n_new).  Everything said at the top of this file holds; unlike the calls above these leave the calling
+ * thread's current HIP device as it was.  A view's `lens` already count the new tokens: user u's are the last n_new[u]
+ * of its lens[u] tokens.
+ */
+
+/*
+ * Rotary positions: of every head's channels, the first 2 * n_pairs turn in pairs, pair j by the angle
+ * theta_j = position[pair_axis[j]] * inv_freq[j]:
+ *   (x0, x1) -> amplitude * (x0 cos theta_j - x1 sin theta_j, x0 sin theta_j + x1 cos theta_j);
+ * the others pass unchanged.  A token has one to three positions (text: one; images and video: time, height, width),
+ * and every pair turns with one of them.  Angles are formed and reduced in 64 bits, cosines and sines in 32, results
+ * are rounded once.
+ */
+typedef struct spd_rope {
+    int32_t n_axes;           /* positions per token: 1..3                                                        */
+    int32_t n_pairs;          /* pairs that turn: a multiple of 8, 8 .. head_dim / 2                              */
+    int32_t adjacent;         /* 0: pair j is channels (j, j + n_pairs); 1: channels (2j, 2j + 1)                 */
+    const uint8_t *pair_axis; /* HOST [n_pairs], values 0 .. n_axes - 1; NULL: every pair turns with axis 0       */
+    const float *inv_freq;    /* DEVICE [n_pairs] radians per unit of position                                    */
+    float amplitude;          /* multiplies cosines and sines; 1 in the usual case, finite                        */
+} spd_rope;
+
+/*
+ * Turns the n_heads heads of every token of x into y (which may be x itself: in place; otherwise they must not
+ * overlap).
+ *   positions  DEVICE int32 [n_axes][n_tokens], any values
+ *   x, y       DEVICE [n_tokens][n_heads][head_dim] of dtype, 16-byte aligned, the tokens x_token_stride / y_token_stride
+ *              elements apart (multiples of 16 bytes, at least n_heads * head_dim; in place: the same)
+ *   transposed 1: the transposed map (angles of the other sign): the forward map's gradient, and with amplitude 1 its
+ *              inverse.  0: the map above.
+ * n_heads up to 65535; head_dim 64 or 128.
+ */
+int spd_rotate(spd_ctx *ctx, int32_t dtype, int32_t head_dim, const spd_rope *rope, int32_t n_tokens,
+               const int32_t *positions, int32_t n_heads, const void *x, int64_t x_token_stride, void *y,
+               int64_t y_token_stride, int32_t transposed, void *hip_stream);
+
+/*
+ * Appends the new tokens to a cache: their keys, turned by `rope` on the way (NULL: as they are), and their values
+ * become tokens lens[u] - n_new[u] .. lens[u] - 1 of user u's buffers or pages; with q and q_out (both or neither) the
+ * tokens' queries are turned in the same launch.  Nothing else is written.
+ *   n_new      HOST [n_users], 0 .. lens[u]
+ *   positions  DEVICE int32 [n_axes][T], or NULL without a rope
+ *   q          DEVICE [T][Hq][d], the tokens q_token_stride elements apart; q_out DEVICE [T][Hq][d] dense (may be q if
+ *              that is dense too)
+ *   k_new, v_new  DEVICE [T][Hkv][d], the tokens k_token_stride / v_token_stride elements apart
+ * Token strides are multiples of 16 bytes and at least a token's heads, so a projection's [T][(Hq + 2 Hkv) * d] result
+ * can be passed as three pointers into it.  Contiguous buffers must have room for lens[u] tokens; the block table must
+ * name the pages of the new positions, and no two users may append to one page's same place.
+ */
+int spd_append_tokens(spd_ctx *ctx, const spd_shape *shape, const spd_kv_view *view, const int32_t *n_new,
+                      const spd_rope *rope, const int32_t *positions, const void *q, int64_t q_token_stride, void *q_out,
+                      const void *k_new, int64_t k_token_stride, const void *v_new, int64_t v_token_stride,
+                      void *hip_stream);
+
+/*
+ * What lies between <q, k> and the softmax, and which keys a query sees.  All zero / NULL: every key, scaled products.
+ *   s = scale * <q, k>;   s = cap * tanh(s / cap) if cap > 0;   s -= slopes[h] * |pos_q - pos_k| if slopes
+ * A key of the view has position k_pos[u] + its index; user u's new token i has position q_pos[u] + i.  These count
+ * tokens of the sequence (a rotary position may be something else).  A query sees the keys of its user with
+ *   ranges[2t] <= pos_k < ranges[2t + 1]   (t: the query's index among the T tokens; documents)   and
+ *   pos_k < prefix[u]   or   (pos_k <= pos_q if causal, and |pos_q - pos_k| < window if window > 0).
+ * A query that sees no key has A = 0 and lse = -inf.  What a key holds that a query does not see - infinities and NaN
+ * among it - does not reach that query's result.  A value that is not finite makes the results of the queries that see it
+ * not finite in its channel (infinite or NaN), and no others.
+ */
+typedef struct spd_score {
+    float cap;              /* 0 (none) or positive, finite                                                         */
+    const float *slopes;    /* DEVICE [Hq] finite, or NULL                                                          */
+    int32_t causal;         /* 0 or 1                                                                               */
+    int32_t window;         /* 0: unlimited, else 1 .. 2^30                                                         */
+    const int32_t *prefix;  /* HOST [n_users], 0 .. 2^30, or NULL: none                                             */
+    const int32_t *ranges;  /* DEVICE [T][2], any values, or NULL: everything                                       */
+    const int32_t *q_pos;   /* HOST [n_users], 0 .. 2^30, or NULL: the view's last positions, k_pos[u] + lens[u] - n_new[u] */
+    const int32_t *k_pos;   /* HOST [n_users], 0 .. 2^30, or NULL: 0                                                */
+} spd_score;
+
+/*
+ * Partial attention of every new token over its user's keys in the view (which need not hold the new tokens: with q_pos
+ * given, lens may be anything, so that tokens appended to one owner's cache attend to the other owner's too; the two
+ * partials merge with spd_lse_merge):
+ *   A[t][h] = sum_k exp(s_k - lse) v_k,   lse[t][h] = ln sum_k exp(s_k)   over the keys that the query sees.
+ *   n_new      HOST [n_users], 0 .. 2^30 (at most lens[u] where q_pos is NULL); T * Hq at most 2^31 - 1
+ *   q          DEVICE [T][Hq][d], the tokens q_token_stride elements apart (as in spd_append_tokens)
+ *   out        DEVICE [T][Hq][d] of out_dtype: SPD_F32, or shape->dtype (each value rounded once; 16-bit probabilities
+ *              then enter the second product rounded once too)
+ *   lse        DEVICE [T][Hq] fp32
+ *   score      NULL: all zero
+ * Few rows over long caches are split over the keys and joined; many go through matrix tiles.  The same graph rules as
+ * for the partial calls above: run a call once eagerly before it is recorded (a call that has to build its schedule or
+ * grow scratch memory under capture fails with SPD_ERR_HIP).  What a recorded call uses of the context is kept for it
+ * until spd_destroy, but it shares scratch memory with later calls of this entry point: they must not overlap in time.
+ */
+int spd_partial_attn_tokens(spd_ctx *ctx, const spd_shape *shape, const void *q, int64_t q_token_stride,
+                            const spd_kv_view *view, const int32_t *n_new, const spd_score *score, void *out,
+                            int32_t out_dtype, float *lse, void *hip_stream);
+
+/* The validation that spd_partial_attn_tokens and spd_append_tokens perform first (host only, no GPU needed). */
+int spd_validate_tokens(const spd_shape *shape, const void *q, int64_t q_token_stride, const spd_kv_view *view,
+                        const int32_t *n_new, const spd_score *score, const void *out, int32_t out_dtype,
+                        const float *lse);
+int spd_validate_append(const spd_shape *shape, const spd_kv_view *view, const int32_t *n_new, const spd_rope *rope,
+                        const int32_t *positions, const void *q, int64_t q_token_stride, const void *q_out,
+                        const void *k_new, int64_t k_token_stride, const void *v_new, int64_t v_token_stride);
+int spd_validate_rotate(int32_t dtype, int32_t head_dim, const spd_rope *rope, int32_t n_tokens,
+                        const int32_t *positions, int32_t n_heads, const void *x, int64_t x_token_stride, const void *y,
+                        int64_t y_token_stride);
+
 #ifdef __cplusplus
 }
 #endif

@@ -29,7 +29,8 @@ EXPORTED_SYMBOLS = (
     "spd_decode_step", "spd_partial_attn_public_batched_append", "spd_get_schedule_stats",
     "spd_attention_mass_track", "spd_get_kernel_timing_samples", "spd_lse_merge_n", "spd_public_attn_merge",
     "spd_abi_version", "spd_decode_step_static", "spd_set_option", "spd_get_option",
-    "spd_get_last_kernel_instance",
+    "spd_get_last_kernel_instance", "spd_rotate", "spd_append_tokens", "spd_partial_attn_tokens",
+    "spd_validate_rotate", "spd_validate_append", "spd_validate_tokens",
 )
 
 SPD_ABI_VERSION = 4      # include/spd.h's; checked against the loaded library below
@@ -56,6 +57,16 @@ class spd_kv_view(C.Structure):
                 ("k_pool", C.c_void_p), ("v_pool", C.c_void_p), ("block_size", C.c_int32),
                 ("block_table", C.c_void_p), ("max_blocks", C.c_int32), ("block_stride", C.c_int64),
                 ("k_ptrs_dev", C.c_void_p), ("v_ptrs_dev", C.c_void_p)]
+
+
+class spd_rope(C.Structure):
+    _fields_ = [("n_axes", C.c_int32), ("n_pairs", C.c_int32), ("adjacent", C.c_int32), ("pair_axis", C.c_void_p),
+                ("inv_freq", C.c_void_p), ("amplitude", C.c_float)]
+
+
+class spd_score(C.Structure):
+    _fields_ = [("cap", C.c_float), ("slopes", C.c_void_p), ("causal", C.c_int32), ("window", C.c_int32),
+                ("prefix", C.c_void_p), ("ranges", C.c_void_p), ("q_pos", C.c_void_p), ("k_pos", C.c_void_p)]
 
 
 class spd_work_item(C.Structure):
@@ -122,6 +133,20 @@ def _load() -> C.CDLL:
     lib.spd_build_schedule.argtypes = [C.POINTER(spd_shape), C.c_int32, C.POINTER(C.c_int32), C.c_int32, C.c_int32,
                                        C.POINTER(spd_work_item), C.c_int64, C.POINTER(C.c_int64),
                                        C.POINTER(C.c_int32)]
+    i32, i64 = C.c_int32, C.c_int64
+    rope, score, shape, view = C.POINTER(spd_rope), C.POINTER(spd_score), C.POINTER(spd_shape), C.POINTER(spd_kv_view)
+    rotate = [i32, i32, rope, i32, vp, i32, vp, i64, vp, i64]
+    lib.spd_rotate.argtypes = [vp, *rotate, i32, vp]
+    lib.spd_validate_rotate.argtypes = rotate
+    append = [shape, view, vp, rope, vp, vp, i64, vp, vp, i64, vp, i64]
+    lib.spd_append_tokens.argtypes = [vp, *append, vp]
+    lib.spd_validate_append.argtypes = append
+    tokens = [shape, vp, i64, view, vp, score, vp, i32, fp]
+    lib.spd_partial_attn_tokens.argtypes = [vp, *tokens, vp]
+    lib.spd_validate_tokens.argtypes = tokens
+    for name in ("spd_rotate", "spd_append_tokens", "spd_partial_attn_tokens", "spd_validate_rotate", "spd_validate_append",
+                 "spd_validate_tokens"):
+        getattr(lib, name).restype = C.c_int
     return lib
 
 
@@ -185,6 +210,72 @@ class KVView:
                        block_table=side.block_table, block_size=side.page_tokens, block_stride=side.block_stride)
         return cls(side.lens, side.token_stride, side.head_stride, k=side.k, v=side.v,
                    head_strides=getattr(side, "head_strides", None), device_pointer_tables=device_pointer_tables)
+
+
+_DTYPE_CODES = {torch.float32: SPD_F32, torch.bfloat16: SPD_BF16, torch.float16: SPD_F16}
+_CODE_DTYPES = {code: dtype for dtype, code in _DTYPE_CODES.items()}
+
+
+class Rope:
+    """Marshalled spd_rope: pair j of a head's channels turns by position[pair_axis[j]] * inv_freq[j] (inv_freq: fp32 on the GPU,
+    one entry per pair); keeps the arrays alive."""
+
+    def __init__(self, inv_freq: torch.Tensor, n_axes: int = 1, pair_axis=None, adjacent: bool = False, amplitude: float = 1.0):
+        assert inv_freq.dtype is torch.float32 and inv_freq.is_contiguous() and inv_freq.dim() == 1
+        st = spd_rope()
+        st.n_axes, st.n_pairs, st.adjacent, st.amplitude = int(n_axes), int(inv_freq.numel()), int(bool(adjacent)), float(amplitude)
+        if pair_axis is not None:
+            self.pair_axis = np.ascontiguousarray(pair_axis, dtype=np.uint8)
+            assert self.pair_axis.shape == (inv_freq.numel(),)
+            st.pair_axis = self.pair_axis.ctypes.data
+        st.inv_freq = inv_freq.data_ptr()
+        self.inv_freq = inv_freq
+        self.struct = st
+
+
+class Score:
+    """Marshalled spd_score: cap, bias by distance and masks of a partial attention; keeps the arrays alive.  prefix, q_pos and k_pos are
+    host sequences with an entry per user, slopes (fp32 [Hq]) and ranges (int32 [T, 2]) tensors on the GPU."""
+
+    def __init__(self, cap: float = 0.0, slopes: Optional[torch.Tensor] = None, causal: bool = True, window: int = 0, prefix=None,
+                 ranges: Optional[torch.Tensor] = None, q_pos=None, k_pos=None):
+        st = spd_score()
+        st.cap, st.causal, st.window = float(cap), int(bool(causal)), int(window)
+        if slopes is not None:
+            assert slopes.dtype is torch.float32 and slopes.is_contiguous() and slopes.dim() == 1
+            st.slopes = slopes.data_ptr()
+        if ranges is not None:
+            assert ranges.dtype is torch.int32 and ranges.is_contiguous() and ranges.dim() == 2 and ranges.shape[1] == 2
+            st.ranges = ranges.data_ptr()
+        self.slopes, self.ranges, self.per_user = slopes, ranges, {}
+        for name, given in (("prefix", prefix), ("q_pos", q_pos), ("k_pos", k_pos)):
+            if given is not None:
+                self.per_user[name] = np.ascontiguousarray(given, dtype=np.int32)
+                assert self.per_user[name].ndim == 1
+                setattr(st, name, self.per_user[name].ctypes.data)
+        self.struct = st
+
+    def check(self, n_users: int, n_tokens: int, n_q_heads: int):
+        assert all(a.shape == (n_users,) for a in self.per_user.values())
+        assert self.slopes is None or self.slopes.numel() == n_q_heads
+        assert self.ranges is None or self.ranges.shape[0] == n_tokens
+
+
+def _new_counts(n_new, n_users: int):
+    """(host int32 array, sum) of the users' new tokens."""
+    counts = np.ascontiguousarray(n_new, dtype=np.int32)
+    assert counts.shape == (n_users,)
+    return counts, int(counts.sum(dtype=np.int64))
+
+
+def _token_rows(t: torch.Tensor, n_tokens: int, n_heads: int, head_dim: int) -> int:
+    """The token stride of a [T][heads][d] tensor whose heads lie end to end."""
+    assert t.dim() == 3 and t.shape == (n_tokens, n_heads, head_dim)
+    if n_tokens <= 1:      # (torch may give a dimension of one any stride)
+        assert n_tokens == 0 or t[0].is_contiguous()
+        return n_heads * head_dim
+    assert t.stride(2) == 1 and (n_heads == 1 or t.stride(1) == head_dim)
+    return t.stride(0)
 
 
 # torch's current stream as a pointer, without the Stream object around it (2 us of a call that takes 11) where torch offers that
@@ -405,6 +496,62 @@ class Context:
                                  None if w_out is None else w_out.data_ptr(), _stream_ptr(stream))
         self._check(rc, "spd_lse_merge_n")
         return y
+
+    def spd_rotate(self, rope: Rope, x: torch.Tensor, positions: torch.Tensor, y: Optional[torch.Tensor] = None, transposed: bool = False,
+                   stream=None):
+        """Rotary positions on x [T][heads][d] (heads end to end; tokens may be further apart) into y (default: a new tensor; x itself turns
+        in place).  positions: int32 [axes][T] (or [T] with one axis)."""
+        T, H, d = x.shape
+        if y is None:
+            y = torch.empty((T, H, d), device=x.device, dtype=x.dtype)
+        assert y.dtype == x.dtype and y.device == x.device
+        assert positions.dtype is torch.int32 and positions.is_contiguous() and positions.numel() == rope.struct.n_axes * T
+        rc = lib.spd_rotate(self.handle, _DTYPE_CODES[x.dtype], d, C.byref(rope.struct), T, positions.data_ptr(), H, x.data_ptr(),
+                            _token_rows(x, T, H, d), y.data_ptr(), _token_rows(y, T, H, d), int(bool(transposed)), _stream_ptr(stream))
+        self._check(rc, "spd_rotate")
+        return y
+
+    def spd_append_tokens(self, shape, view: KVView, n_new, k_new, v_new, rope: Optional[Rope] = None, positions=None, q=None, q_out=None,
+                          stream=None):
+        """The new tokens' keys (turned by rope) and values into the view's cache, whose lengths already count them; q, if given, turned
+        beside them into q_out (default: a new tensor), which is returned."""
+        counts, T = _new_counts(n_new, view.struct.n_users)
+        Hq, H, d, dtype = shape.n_q_heads, shape.n_kv_heads, shape.head_dim, _CODE_DTYPES[shape.dtype]
+        ks, vs, qs = _token_rows(k_new, T, H, d), _token_rows(v_new, T, H, d), 0
+        assert k_new.dtype == v_new.dtype == dtype
+        assert rope is None or (positions.dtype is torch.int32 and positions.is_contiguous() and positions.numel() == rope.struct.n_axes * T)
+        if q is not None:
+            qs = _token_rows(q, T, Hq, d)
+            if q_out is None:
+                q_out = torch.empty((T, Hq, d), device=q.device, dtype=dtype)
+            assert q.dtype == q_out.dtype == dtype and q_out.is_contiguous() and q_out.shape == (T, Hq, d)
+        rc = lib.spd_append_tokens(self.handle, C.byref(shape), C.byref(view.struct), counts.ctypes.data,
+                                   None if rope is None else C.byref(rope.struct), None if rope is None else positions.data_ptr(),
+                                   None if q is None else q.data_ptr(), qs, None if q is None else q_out.data_ptr(), k_new.data_ptr(), ks,
+                                   v_new.data_ptr(), vs, _stream_ptr(stream))
+        self._check(rc, "spd_append_tokens")
+        return q_out if q is not None else None
+
+    def spd_partial_attn_tokens(self, shape, q, view: KVView, n_new, score: Optional[Score] = None, out=None, lse=None, out_dtype=None,
+                                stream=None):
+        """Partial attention of every user's n_new[u] tokens (q: [T][Hq][d]) over its keys in the view.  out: [T][Hq][d] in fp32 or the
+        inputs' type (out_dtype where out is not given; default fp32).  Returns (out, lse)."""
+        counts, T = _new_counts(n_new, view.struct.n_users)
+        Hq, d, dtype = shape.n_q_heads, shape.head_dim, _CODE_DTYPES[shape.dtype]
+        if out is None:
+            out = torch.empty((T, Hq, d), device=q.device, dtype=out_dtype or torch.float32)
+        if lse is None:
+            lse = torch.empty((T, Hq), device=q.device, dtype=torch.float32)
+        qs = _token_rows(q, T, Hq, d)
+        assert q.dtype == dtype and out.is_contiguous() and out.shape == (T, Hq, d) and out.dtype in (torch.float32, dtype)
+        assert lse.is_contiguous() and lse.shape == (T, Hq) and lse.dtype is torch.float32
+        if score is not None:
+            score.check(view.struct.n_users, T, Hq)
+        rc = lib.spd_partial_attn_tokens(self.handle, C.byref(shape), q.data_ptr(), qs, C.byref(view.struct), counts.ctypes.data,
+                                         None if score is None else C.byref(score.struct), out.data_ptr(), _DTYPE_CODES[out.dtype],
+                                         lse.data_ptr(), _stream_ptr(stream))
+        self._check(rc, "spd_partial_attn_tokens")
+        return out, lse
 
 
 def spd_validate_partial(shape: spd_shape, q_ptr, view: spd_kv_view, out_ptr, lse_ptr) -> int:

@@ -4,6 +4,7 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
@@ -19,16 +20,32 @@ HIPCC_FLAGS = [
 ]
 
 
+SOURCES = ("spd_api.hip", "tokens_api.hip", "tokens_few.hip", "tokens_many.hip")
+
+
 def build_library(verbose: bool = False, extra_flags=()) -> str:
+    """Every source compiled by itself, side by side, and linked."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc, *HIPCC_FLAGS, *extra_flags, "-o", LIB, os.path.join(CSRC, "spd_api.hip")]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     noise = "is not a recognized feature for this target"   # printed by the host pass for the gfx-only flag
-    out = "\n".join(l for l in res.stdout.splitlines() if noise not in l)
-    if res.returncode != 0:
-        raise RuntimeError(f"hipcc failed ({res.returncode}):\n{out}")
+    with tempfile.TemporaryDirectory() as tmp:
+        jobs = []
+        for src in SOURCES:
+            obj = os.path.join(tmp, src + ".o")
+            cmd = [hipcc, *(f for f in HIPCC_FLAGS if f != "-shared"), *extra_flags, "-c", "-o", obj, os.path.join(CSRC, src)]
+            if verbose:
+                print(" ".join(cmd), flush=True)
+            jobs.append((obj, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+        results = [(job.communicate()[0], job.returncode) for _, job in jobs]
+        link = [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *(obj for obj, _ in jobs)]
+        if all(rc == 0 for _, rc in results):
+            if verbose:
+                print(" ".join(link), flush=True)
+            res = subprocess.run(link, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+            results.append((res.stdout, res.returncode))
+    out = "\n".join(l for text, _ in results for l in text.splitlines() if noise not in l)
+    bad = [rc for _, rc in results if rc != 0]
+    if bad:
+        raise RuntimeError(f"hipcc failed ({bad[0]}):\n{out}")
     if verbose and out.strip():
         print(out)
     return LIB

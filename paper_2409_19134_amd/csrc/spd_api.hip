@@ -17,6 +17,7 @@
 
 #include "combine.hpp"
 #include "common.hpp"
+#include "context.hpp"
 #include "host_checks.hpp"
 #include "partial_mfma.hpp"
 #include "schedule.hpp"
@@ -79,10 +80,7 @@ struct Owner {
 
 }  // namespace
 
-struct spd_ctx {
-    int device = 0;
-    int n_cus = 0;
-    int last_hip = 0;
+struct spd_ctx : spd::ContextBase {
     uint64_t tick = 0;
     int64_t schedule_builds = 0, schedule_hits = 0;
     bool timing = false;
@@ -1221,6 +1219,10 @@ int no_throw(F &&body)
 
 }  // namespace
 
+namespace spd {
+ContextBase *context_base(spd_ctx *ctx) { return ctx; }
+}  // namespace spd
+
 extern "C" {
 
 int spd_abi_version(void) { return SPD_ABI_VERSION; }
@@ -1289,6 +1291,8 @@ int spd_destroy(spd_ctx *ctx)
         return SPD_ERR_NULL;
     (void)hipSetDevice(ctx->device);
     (void)hipDeviceSynchronize();
+    if (ctx->tokens)
+        ctx->tokens_free(ctx->tokens);
     for (auto &own : ctx->owner) {
         for (auto &e : own.cache)
             free_entry(e);

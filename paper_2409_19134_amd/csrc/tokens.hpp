@@ -1,0 +1,253 @@
+// Shared declarations of the calls for several new tokens per user: the tables that the host builds and the kernels read,
+// the kernels' arguments, and what happens to a score between <q, k> and the softmax.
+#pragma once
+#include "common.hpp"
+
+namespace spd {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// A user as the kernels read it, indexed by user.  Positions are relative to the view's first key.
+struct TokUser {
+    const char *k_base, *v_base;  // contiguous without device pointer tables: the user's buffers; else nullptr
+    int64_t head_stride;          // bytes
+    int32_t tok0, n_tok;          // its first new token among all, and how many
+    int32_t len;                  // keys (grows with TokArgs::grow_len)
+    int32_t q_pos;                // position of its first new token (grows with grow_q)
+    int32_t prefix;               // keys below it are seen by every query
+    int32_t k_pos;                // position of key 0, for the ranges
+    int32_t pad[4];
+};
+static_assert(sizeof(TokUser) == 64);
+
+// A tile of query rows (row = token * G + query head of the group, counted from the user's first token) over a stretch of its keys.
+struct TokItem {
+    int32_t user, kv_head;
+    int32_t row0, n_rows;
+    int32_t k_begin, k_end;  // k_begin is a multiple of the kernel's step; so is k_end unless it is the view's length
+    int32_t slot;            // where its partial goes, or -1: it writes the result
+    int32_t to_len;          // 1: k_end is the view's length (grows with it)
+};
+static_assert(sizeof(TokItem) == 32);
+
+// A tile whose keys were split: partials slot .. slot + n_chunks - 1.
+struct TokJoin {
+    int32_t user, kv_head, row0, n_rows, slot, n_chunks, pad[2];
+};
+static_assert(sizeof(TokJoin) == 32);
+
+struct ScoreArgs {
+    float c;                  // |scale| log2(e)
+    float cap_in, cap_out;    // |scale| / cap, cap log2(e); cap_out 0: no cap
+    uint32_t q_and, q_xor;    // applied to the queries' bits: 0 for scale 0 (c is then 1), the sign bits for a negative scale
+    const float *slopes;      // [Hq] or nullptr
+    const int32_t *ranges;    // [T][2] or nullptr
+    int32_t causal, window;
+};
+
+struct TokArgs {
+    const TokItem *items;
+    const TokUser *users;
+    const char *q;
+    int64_t q_stride;                  // bytes between tokens
+    const char *const *k_ptrs;         // device pointer tables, or nullptr
+    const char *const *v_ptrs;
+    const char *k_pool, *v_pool;       // paged, else nullptr
+    const int32_t *block_table;
+    int64_t block_stride, token_stride;  // bytes
+    int32_t max_blocks, page_shift;
+    int32_t Hq, G;
+    int32_t grow_len, grow_q;
+    char *out;
+    int32_t out_f32;
+    float *lse;
+    float *part_o;    // [slot][rows of a tile][D]
+    float2 *part_lse; // [slot][rows of a tile]: log2 of the sum, and what the final lse adds to it (natural log)
+    ScoreArgs score;
+};
+
+// A query row's masks and bias.  It sees the keys in [mlo, mlo + mn) and in [plo, plo + pn).
+struct RowMask {
+    int mlo, plo;
+    unsigned mn, pn;
+    int q_pos;
+    int dist0;      // its distance to the nearest key it sees: the bias is taken relative to that one, so that far rows lose nothing
+    float slope2;   // slope log2(e)
+    float slope;
+};
+
+__host__ __device__ __forceinline__ int clampi(int v, int lo, int hi) { return min(max(v, lo), hi); }
+
+__host__ __device__ __forceinline__ RowMask row_mask(const ScoreArgs &s, const TokUser &u, int len, int q_pos, int token, int head)
+{
+    RowMask r;
+    int rlo = 0, rhi = len;
+    if (s.ranges) {  // positions; those of keys are not negative
+        const int2 v = reinterpret_cast<const int2 *>(s.ranges)[u.tok0 + token];
+        rlo = max(max(v.x, 0) - u.k_pos, 0);
+        rhi = min(max(v.y, 0) - u.k_pos, len);
+    }
+    int wlo = rlo, whi = rhi;
+    if (s.window) {
+        wlo = max(rlo, q_pos - s.window + 1);
+        if (!s.causal)
+            whi = min(rhi, q_pos + s.window);
+    }
+    if (s.causal)
+        whi = min(rhi, q_pos + 1);
+    r.mlo = wlo;
+    r.mn = (unsigned)max(whi - wlo, 0);
+    r.plo = rlo;
+    r.pn = (unsigned)max(min(rhi, u.prefix) - rlo, 0);
+    r.q_pos = q_pos;
+    r.dist0 = 0;
+    r.slope = r.slope2 = 0.f;
+    if (s.slopes) {
+        r.slope = s.slopes[head];
+        r.slope2 = r.slope * kLog2e;
+        int d = 0x7fffffff;
+        if (r.mn)
+            d = abs(q_pos - clampi(q_pos, r.mlo, r.mlo + (int)r.mn - 1));
+        if (r.pn)
+            d = min(d, abs(q_pos - clampi(q_pos, r.plo, r.plo + (int)r.pn - 1)));
+        r.dist0 = d == 0x7fffffff ? 0 : d;
+    }
+    return r;
+}
+
+__host__ __device__ __forceinline__ bool sees(const RowMask &r, int key)
+{
+    return (unsigned)(key - r.mlo) < r.mn || (unsigned)(key - r.plo) < r.pn;
+}
+
+// tanh from its definition by one exponential, (1 - e) / (1 + e) with e = exp(-2|x|): off by a few 1e-8 of 1.  PRECISE: near zero, where that is
+// much of the value, the series instead (x^13's term is 2e-9 of x at 0.3).
+template <bool PRECISE>
+__device__ __forceinline__ float tanh_of(float x)
+{
+    const float a = fabsf(x);
+    const float e = fast_exp2(-2.f * kLog2e * a);
+    float t = copysignf((1.f - e) * fast_rcp(1.f + e), x);
+    if constexpr (PRECISE) {
+        const float y = x * x;
+        float p = fmaf(y, -1382.f / 155925.f, 62.f / 2835.f);
+        p = fmaf(y, p, -17.f / 315.f);
+        p = fmaf(y, p, 2.f / 15.f);
+        p = fmaf(y, p, -1.f / 3.f);
+        t = a < 0.3f ? fmaf(x * y, p, x) : t;
+    }
+    return t;
+}
+
+// A product <q, k> with its cap and bias, in units of log2 (MOD) or as it is (the factor c comes with the exponential then).
+template <bool MOD, bool PRECISE>
+__device__ __forceinline__ float modified(float s, const ScoreArgs &a, const RowMask &r, int key)
+{
+    if constexpr (!MOD)
+        return s;
+    float x = a.cap_out != 0.f ? tanh_of<PRECISE>(s * a.cap_in) * a.cap_out : s * a.c;
+    if (a.slopes)
+        x = fmaf(-r.slope2, (float)(abs(r.q_pos - key) - r.dist0), x);
+    return x;
+}
+
+// A key that a row does not see must not reach it, and zero times infinity is NaN: where some row does not see some key, non-finite values
+// of V go into the product as zeros, and the rows that do see them get them added afterwards (rare, so from memory again).
+template <int DT>
+__device__ __forceinline__ uint32_t nonfinite(uint32_t dword)  // zero unless one of the dword's values is
+{
+    if constexpr (DT == SPD_F32) {
+        return (dword & 0x7f800000u) == 0x7f800000u ? 1u : 0u;
+    } else {
+        constexpr uint32_t exp = DT == SPD_F16 ? 0x7c007c00u : 0x7f807f80u, one = DT == SPD_F16 ? 0x04000400u : 0x00800080u;
+        return ((dword & exp) + one) & 0x80008000u;
+    }
+}
+template <int DT>
+__device__ __forceinline__ uint32_t finite_part(uint32_t dword)
+{
+    const uint32_t bad = nonfinite<DT>(dword);
+    if constexpr (DT == SPD_F32)
+        return bad ? 0u : dword;
+    else
+        return dword & ~((bad & 0x8000u ? 0xffffu : 0u) | (bad & 0x80000000u ? 0xffff0000u : 0u));
+}
+// Channel `ch` of the row at v if it is not finite, else zero.
+template <int DT>
+__device__ __forceinline__ float nonfinite_part(const char *v, int ch)
+{
+    float x;
+    if constexpr (DT == SPD_F32)
+        x = reinterpret_cast<const float *>(v)[ch];
+    else if constexpr (DT == SPD_BF16)
+        x = (float)reinterpret_cast<const __bf16 *>(v)[ch];
+    else
+        x = (float)reinterpret_cast<const _Float16 *>(v)[ch];
+    return nonfinite<SPD_F32>(__float_as_uint(x)) ? x : 0.f;
+}
+
+// Offset of a user's token in its cache (table: its row of the block table, nullptr: contiguous).
+__device__ __forceinline__ int64_t token_offset(const TokArgs &a, const int32_t *table, int t)
+{
+    if (table)
+        return (int64_t)table[t >> a.page_shift] * a.block_stride + (int64_t)(t & ((1 << a.page_shift) - 1)) * a.token_stride;
+    return (int64_t)t * a.token_stride;
+}
+
+// Base addresses of a user's head.
+__device__ __forceinline__ void kv_bases(const TokArgs &a, const TokUser &u, int user, int kv_head, const char *&k, const char *&v)
+{
+    const int64_t off = (int64_t)kv_head * u.head_stride;
+    if (a.k_pool) {
+        k = a.k_pool + off;
+        v = a.v_pool + off;
+    } else if (a.k_ptrs) {
+        k = reinterpret_cast<const char *>(user_base(a.k_ptrs, user)) + off;
+        v = reinterpret_cast<const char *>(user_base(a.v_ptrs, user)) + off;
+    } else {
+        k = u.k_base + off;
+        v = u.v_base + off;
+    }
+}
+
+template <class T>
+__device__ __forceinline__ T scalar_load(const T *p, int idx)
+{
+    static_assert(sizeof(T) % 4 == 0);
+    T r;
+    const const_u32_ptr w = (const_u32_ptr)(uintptr_t)(p + idx);
+    uint32_t words[sizeof(T) / 4];
+#pragma unroll
+    for (unsigned i = 0; i < sizeof(T) / 4; ++i)
+        words[i] = w[i];
+    __builtin_memcpy(&r, words, sizeof r);
+    return r;
+}
+
+// Four consecutive channels of a result row, from the normalised sums.
+template <int DT>
+__device__ __forceinline__ void store4(const TokArgs &a, int64_t at, f32x4 v)
+{
+    if (a.out_f32) {
+        *reinterpret_cast<f32x4 *>(a.out + at * 4) = v;
+    } else if constexpr (DT == SPD_BF16) {
+        typedef __bf16 b4 __attribute__((ext_vector_type(4)));
+        b4 w = {(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+        *reinterpret_cast<b4 *>(a.out + at * 2) = w;
+    } else if constexpr (DT == SPD_F16) {
+        typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+        h4 w = {(_Float16)v[0], (_Float16)v[1], (_Float16)v[2], (_Float16)v[3]};
+        *reinterpret_cast<h4 *>(a.out + at * 2) = w;
+    }
+}
+
+// Launches (host): `rows` is the row capacity of the few kernel's tiles, 16 or 32.
+__attribute__((visibility("hidden"))) void launch_tokens_few(int dtype, int head_dim, bool paged, int rows, bool modified, int64_t n_items,
+                                                             const TokArgs &a, hipStream_t stream);
+__attribute__((visibility("hidden"))) void launch_tokens_many(int dtype, int head_dim, bool modified, int64_t n_items, const TokArgs &a,
+                                                              hipStream_t stream);
+constexpr int kManyRows = 128;  // rows of a tile of the many kernel
+__host__ __device__ constexpr int many_keys(int dtype) { return dtype == SPD_F32 ? 32 : 64; }  // keys of its steps
+constexpr int kFewKeys = 32;    // keys that the few kernel's stretches are multiples of
+
+}  // namespace spd

@@ -4,9 +4,10 @@ Pure call sequencing over the C ABI; holds the output buffers so a step allocate
 """
 from __future__ import annotations
 
+import numpy as np
 import torch
 
-from .binding import Context, KVView, make_shape
+from .binding import Context, KVView, Rope, Score, make_shape
 
 
 class DecodeStep:
@@ -131,3 +132,43 @@ class DecodeStep:
         main.wait_event(join)
         c.spd_lse_merge(self.a_in, self.lse_in, self.a_out, self.lse_out, self.y, self.lse, self.w_in, main)
         return self.y
+
+
+class TokenStep:
+    """Several new tokens per user through one layer's caches: a prompt (or a chunk of one) into the cache that holds it, or tokens that follow a
+    prompt in another owner's cache (one each, or several that are to be checked at once).
+
+    `view` is the cache that takes the tokens: its lengths already count them, n_new[u] of user u.  With `prompt` (the other owner's view of
+    the same users) the sequence begins there: the tokens attend to both caches, and the two partials are merged as in Theorem 1.  `rope`, and the
+    keywords of Score that concern a sequence (cap, slopes, causal, window, prefix, ranges), are the model's.  Holds the result buffers."""
+
+    def __init__(self, ctx: Context, dtype, n_q_heads: int, n_kv_heads: int, head_dim: int, scale: float, view: KVView, n_new,
+                 rope: Rope = None, prompt: KVView = None, device="cuda:0", **score):
+        self.ctx, self.view, self.prompt, self.rope = ctx, view, prompt, rope
+        self.shape = make_shape(dtype, n_q_heads, n_kv_heads, head_dim, scale)
+        self.n_new = np.ascontiguousarray(n_new, dtype=np.int32)
+        T = int(self.n_new.sum())
+        f32 = dict(device=device, dtype=torch.float32)
+        self.q = torch.empty((T, n_q_heads, head_dim), device=device, dtype=dtype)
+        self.a_out, self.lse_out = torch.empty((T, n_q_heads, head_dim), **f32), torch.empty((T, n_q_heads), **f32)
+        begin = None if prompt is None else prompt.lens
+        self.score_out = Score(k_pos=begin, **score)
+        if prompt is not None:
+            assert prompt.struct.n_users == view.struct.n_users
+            self.a_in, self.y = (torch.empty((T, n_q_heads, head_dim), **f32) for _ in range(2))
+            self.lse_in, self.lse, self.w_in = (torch.empty((T, n_q_heads), **f32) for _ in range(3))
+            self.score_in = Score(q_pos=begin + view.lens - self.n_new, **score)
+
+    def run(self, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, positions: torch.Tensor = None, stream=None):
+        """Enqueues the step; returns (attention, its log-sum-exp).  q, k_new, v_new: [T][heads][d] as the projection leaves them; positions
+        (with a rope): int32 [axes][T]."""
+        c = self.ctx
+        turned = c.spd_append_tokens(self.shape, self.view, self.n_new, k_new, v_new, self.rope, positions,
+                                     q if self.rope is not None else None, self.q if self.rope is not None else None, stream)
+        q = q if self.rope is None else turned
+        c.spd_partial_attn_tokens(self.shape, q, self.view, self.n_new, self.score_out, self.a_out, self.lse_out, stream=stream)
+        if self.prompt is None:
+            return self.a_out, self.lse_out
+        c.spd_partial_attn_tokens(self.shape, q, self.prompt, self.n_new, self.score_in, self.a_in, self.lse_in, stream=stream)
+        c.spd_lse_merge(self.a_in, self.lse_in, self.a_out, self.lse_out, self.y, self.lse, self.w_in, stream)
+        return self.y, self.lse
