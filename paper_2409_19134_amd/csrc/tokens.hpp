@@ -73,7 +73,6 @@ struct RowMask {
     int q_pos;
     int dist0;      // its distance to the nearest key it sees: the bias is taken relative to that one, so that far rows lose nothing
     float slope2;   // slope log2(e)
-    float slope;
 };
 
 __host__ __device__ __forceinline__ int clampi(int v, int lo, int hi) { return min(max(v, lo), hi); }
@@ -101,10 +100,9 @@ __host__ __device__ __forceinline__ RowMask row_mask(const ScoreArgs &s, const T
     r.pn = (unsigned)max(min(rhi, u.prefix) - rlo, 0);
     r.q_pos = q_pos;
     r.dist0 = 0;
-    r.slope = r.slope2 = 0.f;
+    r.slope2 = 0.f;
     if (s.slopes) {
-        r.slope = s.slopes[head];
-        r.slope2 = r.slope * kLog2e;
+        r.slope2 = s.slopes[head] * kLog2e;
         int d = 0x7fffffff;
         if (r.mn)
             d = abs(q_pos - clampi(q_pos, r.mlo, r.mlo + (int)r.mn - 1));
@@ -119,6 +117,14 @@ __host__ __device__ __forceinline__ bool sees(const RowMask &r, int key)
 {
     return (unsigned)(key - r.mlo) < r.mn || (unsigned)(key - r.plo) < r.pn;
 }
+
+// A row's view of a run of keys from key0 on, made anew for every run: without the detour the compiler keeps every key's differences to the row's
+// limits in registers, over all runs.
+struct RunMask {
+    int m, p, q;
+    __device__ __forceinline__ RunMask(const RowMask &r, int key0) : m(key0 - r.mlo), p(key0 - r.plo), q(r.q_pos - key0) { asm("" : "+v"(m), "+v"(p), "+v"(q)); }
+    __device__ __forceinline__ bool sees(const RowMask &r, int i) const { return (unsigned)(m + i) < r.mn || (unsigned)(p + i) < r.pn; }
+};
 
 // tanh from its definition by one exponential, (1 - e) / (1 + e) with e = exp(-2|x|): off by a few 1e-8 of 1.  PRECISE: near zero, where that is
 // much of the value, the series instead (x^13's term is 2e-9 of x at 0.3).
@@ -139,15 +145,16 @@ __device__ __forceinline__ float tanh_of(float x)
     return t;
 }
 
-// A product <q, k> with its cap and bias, in units of log2 (MOD) or as it is (the factor c comes with the exponential then).
+// A product <q, k> with its cap and bias, in units of log2 (MOD) or as it is (the factor c comes with the exponential then).  apart: the query's position
+// less the key's.
 template <bool MOD, bool PRECISE>
-__device__ __forceinline__ float modified(float s, const ScoreArgs &a, const RowMask &r, int key)
+__device__ __forceinline__ float modified(float s, const ScoreArgs &a, const RowMask &r, int apart)
 {
     if constexpr (!MOD)
         return s;
     float x = a.cap_out != 0.f ? tanh_of<PRECISE>(s * a.cap_in) * a.cap_out : s * a.c;
     if (a.slopes)
-        x = fmaf(-r.slope2, (float)(abs(r.q_pos - key) - r.dist0), x);
+        x = fmaf(-r.slope2, (float)(abs(apart) - r.dist0), x);
     return x;
 }
 

@@ -216,13 +216,14 @@ __global__ __launch_bounds__(256, 2) void tokens_few_kernel(const TokArgs a)
                         }
                     }
                 float x[NE];
+                const RunMask run(mask[nt], t0);
 #pragma unroll
                 for (int e = 0; e < NE; ++e)
-                    x[e] = modified<MOD, true>(s[e / 4][e % 4], a.score, mask[nt], t0 + e);
+                    x[e] = modified<MOD, true>(s[e / 4][e % 4], a.score, mask[nt], run.q - e);
                 if (masked)
 #pragma unroll
                     for (int e = 0; e < NE; ++e)
-                        x[e] = sees(mask[nt], t0 + e) ? x[e] : -INFINITY;
+                        x[e] = run.sees(mask[nt], e) ? x[e] : -INFINITY;
                 float mt = x[0];
 #pragma unroll
                 for (int e = 1; e < NE; ++e)
@@ -336,7 +337,7 @@ __global__ __launch_bounds__(256, 2) void tokens_few_kernel(const TokArgs a)
             float offset = 0.f;
             if (MOD && a.score.slopes && ch == 0) {
                 const RowMask mk = row_mask(a.score, u, len, q_pos0 + token, token, head);
-                offset = -mk.slope * (float)mk.dist0;
+                offset = -a.score.slopes[head] * (float)mk.dist0;
             }
             if (it.slot >= 0) {
                 *reinterpret_cast<f32x4 *>(a.part_o + ((int64_t)it.slot * kRows + nt * 16 + rr) * D + ch) = o;

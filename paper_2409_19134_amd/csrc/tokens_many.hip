@@ -47,21 +47,34 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
 typedef __attribute__((address_space(3))) uint32_t lds_u32;
 
+// Sixteen bytes from every lane's offset behind `from` to its place behind `to` (both the wave's) without a trip through registers.  Not by the builtin: the compiler then waits
+// for all of them in front of every LDS read that it cannot tell from them.  Nothing but all_loads_done() and a barrier orders reads behind them.
+__device__ __forceinline__ void load_to_lds(const char *from, uint32_t lane_off, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(lane_off), "s"(from) : "memory");
+}
+__device__ __forceinline__ uint32_t lds_address(const char *p) { return (uint32_t)uniform((int)(uint32_t)(uintptr_t)(lds_char *)p); }
+__device__ __forceinline__ void all_loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// What happens to a score.  kCapped: a cap alone, for results of 16 bits: two multiplications, an addition, an exponential and a reciprocal, of which
+// the softmax's own multiplication takes the last (the general form, with a copied sign and the bias, takes eleven; prompts of 900-4096 tokens
+// with 32 heads of 128, us per call, general / this: see below).  It is off by 2^-23 of the cap, which 24-bit results would show.
+enum { kPlain = 0, kCapped = 1, kGeneral = 2 };
+
 constexpr float kRaise = 8.f;   // log2 of what a row's largest P may be
 // P carries 2^kShift: fp16's keep to [2^-24, 65504] with a maximum of 2^(kRaise + 7)
 template <int DT>
 constexpr float kShift = DT == SPD_F16 ? 7.f : 0.f;
 
-template <int DT, int D, bool EXACT, bool MOD>
+template <int DT, int D, bool EXACT, int MOD>
 __global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
 {
     constexpr bool kF32 = DT == SPD_F32;
     constexpr int kBytes = kF32 ? 4 : 2, RB = D * kBytes, BN = many_keys(DT), NB = BN / 32, C = RB / 16, KK = RB / 32, CB = D / 32;
     constexpr int kTile = BN * RB, kPieces = BN * C / 256;
     constexpr int kTerms = EXACT ? Block<DT>::kTerms : 1;
-    __shared__ __attribute__((aligned(16))) char lds[2][2][kTile];  // [buffer][K, V]
-    __shared__ int lds_bounds[4][4];
-    __shared__ uint32_t lds_bad[2][4];
+    __shared__ __attribute__((aligned(16))) char k_lds[2][kTile], v_lds[2][kTile];
+    __shared__ int lds_bounds[4][6];
 
     const TokItem it = scalar_load(a.items, blockIdx.x);
     if (it.n_rows == 0)
@@ -114,11 +127,15 @@ __global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
         lds_bounds[wave][1] = my_hi;
         lds_bounds[wave][2] = my_pre;
         lds_bounds[wave][3] = my_win;
+        lds_bounds[wave][4] = full_lo;
+        lds_bounds[wave][5] = full_hi;
     }
     __syncthreads();
-    int lo = 0x7fffffff, hi = 0, gap_lo = 0, gap_hi = 0x7fffffff;
+    int lo = 0x7fffffff, hi = 0, gap_lo = 0, gap_hi = 0x7fffffff, all_lo = 0, all_hi = 0x7fffffff;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
+        all_lo = max(all_lo, lds_bounds[w][4]);
+        all_hi = min(all_hi, lds_bounds[w][5]);
         lo = min(lo, lds_bounds[w][0]);
         hi = max(hi, lds_bounds[w][1]);
         gap_lo = max(gap_lo, lds_bounds[w][2]);
@@ -128,8 +145,10 @@ __global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
     hi = min(k_end, uniform(hi));
     gap_lo = uniform(gap_lo);
     gap_hi = uniform(gap_hi);
+    all_lo = uniform(all_lo);
+    all_hi = uniform(all_hi);
 
-    float mc = -INFINITY, l = 0.f;  // running maximum in units of log2 (both lanes of a row), the lane's part of the sum
+    float mc = -INFINITY, l[2] = {0.f, 0.f};  // running maximum in units of log2 (both lanes of a row), the lane's part of the sum (in two)
     f32x16 acc[CB];
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb)
@@ -142,45 +161,45 @@ __global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
     const int32_t *table = a.k_pool ? a.block_table + (int64_t)it.user * a.max_blocks : nullptr;
     const int t_last = hi - 1;
 
-    u32x4 sk[kPieces], sv[kPieces];
-    auto load = [&](int kt) {
-#pragma unroll
-        for (int j = 0; j < kPieces; ++j) {
-            const int id = j * 256 + tid, t = min(kt + id / C, t_last);
-            const int64_t off = token_offset(a, table, t) + (id % C) * 16;
-            typedef const u32x4 __attribute__((address_space(1))) *global_ptr;
-            sk[j] = *(global_ptr)(uintptr_t)(k_base + off);
-            sv[j] = *(global_ptr)(uintptr_t)(v_base + off);
-        }
+    // A row's pieces of sixteen bytes lie at places xor-ed with this (see above): for sixteen rows in a row all different, and for four rows in a row
+    // different in the bits that tell four neighbouring pieces' groups apart.
+    auto swap = [](int row) __attribute__((always_inline)) {
+        if constexpr (kF32)
+            return row & 7;
+        else
+            return C == 16 ? (row & 3) << 2 | (row >> 2 & 3) : (row >> 1 & 1) << 2 | (row & 1) << 1 | (row >> 2 & 1);
     };
-    auto k_place = [](int row, int c) { return row * RB + ((c ^ (row & (C < 16 ? C - 1 : 15))) * 16); };
-    auto v_place = [](int row, int c) {
-        const int x = kF32 ? (row & 4) << 1 : C == 16 ? (row & 7) << 1 : ((row >> 1) & 3) << 1;
-        return row * RB + ((c ^ x) * 16);
-    };
-    auto store = [&](int buf, bool look) {
-        if (look) {
-            uint32_t any = 0;
+    // A wave's share of a tile: kPieces runs of 64 pieces, kRun rows each (inside one page: they are aligned).  What is xor-ed is the same for all
+    // its runs, so a lane's place in a run stays.
+    constexpr int kRun = 64 / C;
+    const int run_row = lane / C;
+    const uint32_t stride = (uint32_t)a.token_stride, block_stride = (uint32_t)a.block_stride;  // (the host's checks keep them below 2^31)
+    const uint32_t part = ((lane % C) ^ swap(wave * kRun + run_row)) * 16;
+    const uint32_t run_off = (uint32_t)(wave * kRun + run_row) * stride + part;
+    const bool by_offset = !table && stride < (1u << 26);  // (a tile's rows lie less than 2^32 bytes apart)
+    auto load = [&](int kt, int buf) __attribute__((always_inline)) {
+        const uint32_t k_to = lds_address(k_lds[buf]) + wave * 1024, v_to = lds_address(v_lds[buf]) + wave * 1024;
+        if (by_offset && kt + BN <= hi) {
+            const uint64_t row = (uint64_t)(uint32_t)kt * stride;
 #pragma unroll
             for (int j = 0; j < kPieces; ++j)
+                load_to_lds(k_base + row, run_off + j * 4 * kRun * stride, k_to + j * 4096);
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    any |= nonfinite<DT>(sv[j][i]);
-            const bool bad = __builtin_amdgcn_ballot_w64(any != 0) != 0;
-            if (bad)
-#pragma unroll
-                for (int j = 0; j < kPieces; ++j)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        sv[j][i] = finite_part<DT>(sv[j][i]);
-            if (lane == 0)
-                lds_bad[buf][wave] = bad;
+            for (int j = 0; j < kPieces; ++j)
+                load_to_lds(v_base + row, run_off + j * 4 * kRun * stride, v_to + j * 4096);
+            return;
         }
 #pragma unroll
         for (int j = 0; j < kPieces; ++j) {
-            const int id = j * 256 + tid;
-            *reinterpret_cast<u32x4 *>(&lds[buf][0][k_place(id / C, id % C)]) = sk[j];
-            *reinterpret_cast<u32x4 *>(&lds[buf][1][v_place(id / C, id % C)]) = sv[j];
+            const int t = min(kt + j * 4 * kRun + wave * kRun, t_last);
+            uint64_t row;
+            if (table)
+                row = (uint64_t)(uint32_t)scalar_load_i32(table, t >> a.page_shift) * block_stride + (uint64_t)(uint32_t)(t & ((1 << a.page_shift) - 1)) * stride;
+            else
+                row = (uint64_t)(uint32_t)t * stride;
+            const uint32_t off = (uint32_t)min(run_row, t_last - t) * stride + part;  // rows behind the last key re-read it (they are masked)
+            load_to_lds(k_base + row, off, k_to + j * 4096);
+            load_to_lds(v_base + row, off, v_to + j * 4096);
         }
     };
     // tiles that no row sees between the prefixes and the windows are passed over
@@ -190,171 +209,227 @@ __global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
             kt = gap_hi / BN * BN;
         return kt;
     };
-    // a tile that some row of the workgroup may not see whole (wave by wave would do; this is what is known everywhere)
-    __shared__ int lds_full[4][2];
-    if (lane == 0) {
-        lds_full[wave][0] = full_lo;
-        lds_full[wave][1] = full_hi;
-    }
-    __syncthreads();
-    const int all_lo = uniform(max(max(lds_full[0][0], lds_full[1][0]), max(lds_full[2][0], lds_full[3][0])));
-    const int all_hi = uniform(min(min(lds_full[0][1], lds_full[1][1]), min(lds_full[2][1], lds_full[3][1])));
+    // a tile that some row of the workgroup may not see whole
     auto partly = [&](int kt) { return kt < all_lo || kt + BN > all_hi; };
+    const float c = MOD == kPlain ? a.score.c : MOD == kCapped ? 2.f * a.score.cap_out : 1.f, steep = 2.f * kLog2e * a.score.cap_in;
+    // lane parts of the LDS places: K row n, piece 2 kk + h; V (16-bit) keys 4 h + i / 4 of sixteen channels' pieces
+    const int k_lane_ = n * RB + (h ^ swap(n)) * 16;
+    const int vi = lane & 15, v_row = 4 * h + vi / 4, v_piece = ((lane >> 4) & 1) * 2 + ((vi & 3) >> 1);
+    const int v_lane[2] = {v_row * RB + (v_piece ^ swap(v_row)) * 16 + (vi & 1) * 8, (v_row + 8) * RB + (v_piece ^ swap(v_row + 8)) * 16 + (vi & 1) * 8};
 
-    const float c = MOD ? 1.f : a.score.c;
-    // lane parts of the LDS places: K row n, piece 2 kk + h; V (16-bit) keys 4 h + i / 4 of sixteen channels' pieces; V (fp32) channel n
-    const int k_lane = k_place(n, h);
-    const int vi = lane & 15, v_row = 4 * h + vi / 4;
-    const int v_lane = kF32 ? 0 : v_place(v_row, ((lane >> 4) & 1) * 2 + ((vi & 3) >> 1)) + (vi & 1) * 8;
-
-    auto compute = [&](int buf, int kt) {
-        f32x16 s[NB];
-        lds_char *const kp = (lds_char *)&lds[buf][0][0], *const vp = (lds_char *)&lds[buf][1][0];
+    // Pieces of the two products.  K: the rows' pieces kk of 32 keys each; V (16-bit): sixteen keys' V^T of 32 channels, by two transposed reads; V
+    // (fp32): one key's values (of each half of the wave).
+    auto read_k = [&](const char *kbuf, int kk, u32x4 (&f)[NB]) __attribute__((always_inline)) {
+        int k_lane = k_lane_;
+        if constexpr (kF32)  // (sixteen addresses are not worth a register each)
+            asm volatile("" : "+v"(k_lane));
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
+            f[nb] = *(lds_u32x4 *)((lds_char *)kbuf + ((k_lane ^ (kk * 32)) + nb * 32 * RB));
+    };
+    auto multiply_k = [&](const u32x4 (&f)[NB], int kk, f32x16 (&x)[NB]) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                s[nb][i] = 0.f;
+        for (int nb = 0; nb < NB; ++nb) {
+            if constexpr (kF32) {
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk)
+                for (int e = 0; e < 4; ++e)
+                    x[nb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(f[nb][e]), __uint_as_float(q[kk][e]), kk + e ? x[nb] : f32x16{}, 0, 0, 0);
+            } else {
+                typedef typename Block<DT>::vec8 vec8;
+                x[nb] = Block<DT>::mfma(__builtin_bit_cast(vec8, f[nb]), __builtin_bit_cast(vec8, q[kk]), kk ? x[nb] : f32x16{});
+            }
+        }
+    };
+    constexpr int kSteps = kF32 ? 16 * NB : 2 * NB;  // of the second product: a key (of each half), or sixteen
+    typedef std::conditional_t<kF32, uint32_t, u32x4> vpiece;
+    auto read_v = [&](const char *vbuf, int m, vpiece (&f)[CB]) __attribute__((always_inline)) {
+        lds_char *const vp = (lds_char *)vbuf;
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
-                const u32x4 w = *(lds_u32x4 *)(kp + ((k_lane ^ (kk * 32)) + nb * 32 * RB));
-                if constexpr (kF32) {
+        for (int cb = 0; cb < CB; ++cb) {
+            if constexpr (kF32) {
+                int key = 8 * (m / 4) + 4 * h + m % 4;
+                asm volatile("" : "+v"(key));
+                f[cb] = *(lds_u32 *)(vp + (key * RB + ((cb * 8 + n / 4) ^ swap(key)) * 16 + n % 4 * 4));
+            } else {
+                union {
+                    s16x4 half[2];
+                    u32x4 w;
+                } r;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        s[nb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(w[e]), __uint_as_float(q[kk][e]), s[nb], 0, 0, 0);
-                } else {
-                    typedef typename Block<DT>::vec8 vec8;
-                    s[nb] = Block<DT>::mfma(__builtin_bit_cast(vec8, w), __builtin_bit_cast(vec8, q[kk]), s[nb]);
+                for (int i = 0; i < 2; ++i)
+                    r.half[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(vp + ((v_lane[i] ^ (cb * 64)) + 16 * m * RB)));
+                f[cb] = r.w;
+            }
+        }
+    };
+    auto multiply_v = [&](const vpiece (&f)[CB], int m, const f32x16 (&p)[NB]) __attribute__((always_inline)) {
+        if constexpr (kF32) {
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb)
+                acc[cb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(f[cb]), p[m / 16][m % 16], acc[cb], 0, 0, 0);
+        } else {
+            typedef typename Block<DT>::vec8 vec8;
+            typedef typename Block<DT>::type E;
+            vec8 w[kTerms];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float left = p[m / 2][8 * (m & 1) + e];
+#pragma unroll
+                for (int t = 0; t < kTerms; ++t) {
+                    w[t][e] = (E)left;
+                    left -= (float)w[t][e];
                 }
             }
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+                for (int t = 0; t < kTerms; ++t)
+                    acc[cb] = Block<DT>::mfma(__builtin_bit_cast(vec8, f[cb]), w[t], acc[cb]);
+        }
+    };
+    // Scores i0 .. i1 of a tile become weights.
+    auto weigh = [&](f32x16 (&p)[NB], int i0, int i1) __attribute__((always_inline)) {
+        const float m_p = (mc == -INFINITY ? 0.f : mc) - kShift<DT>;
+#pragma unroll
+        for (int i = i0; i < i1; ++i) {
+            p[i / 16][i % 16] = fast_exp2(fmaf(p[i / 16][i % 16], c, -m_p));
+            l[i % 2] += p[i / 16][i % 16];
+        }
+    };
+    auto top_of = [&](const f32x16 (&x)[NB], int i0, int i1, float m) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = i0; i < i1; ++i)
+            m = fmaxf(m, x[i / 16][i % 16]);
+        return m;
+    };
+    // Cap, bias and masks of the tile at kt, and the running maximum with them (top: the lane's largest score as it came).
+    auto masks = [&](f32x16 (&x)[NB], int kt, float top) __attribute__((always_inline)) {
+        const RunMask run(mask, kt + 4 * h);
         const bool masked = kt < full_lo || kt + BN > full_hi;
-        const int key0 = kt + 4 * h;
-        if constexpr (MOD)
+        if constexpr (MOD != kPlain)
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    s[nb][i] = modified<true, EXACT>(s[nb][i], a.score, mask, key0 + nb * 32 + 8 * (i / 4) + i % 4);
+                for (int i = 0; i < 16; ++i) {
+                    if constexpr (MOD == kCapped)  // -1 / (1 + exp(2 s / cap)): twice the cap times that, and the cap, is cap tanh(s / cap)
+                        x[nb][i] = fast_rcp(-1.f - fast_exp2(x[nb][i] * steep));
+                    else
+                        x[nb][i] = modified<true, EXACT>(x[nb][i], a.score, mask, run.q - (nb * 32 + 8 * (i / 4) + i % 4));
+                }
         if (masked)
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    s[nb][i] = sees(mask, key0 + nb * 32 + 8 * (i / 4) + i % 4) ? s[nb][i] : -INFINITY;
-        float mt = s[0][0];
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                mt = fmaxf(mt, s[nb][i]);
-        mt = wave_xor_max<32>(mt) * c;
+                    x[nb][i] = run.sees(mask, nb * 32 + 8 * (i / 4) + i % 4) ? x[nb][i] : -INFINITY;
+        if (MOD != kPlain || masked)
+            top = top_of(x, 0, 16 * NB, -INFINITY);
+        const float mt = wave_xor_max<32>(top) * c;
         if (__builtin_amdgcn_ballot_w64(mt > mc + kRaise) != 0) {  // (mc is -inf at first)
             const float m_new = fmaxf(mc, mt);
             const float alpha = m_new == -INFINITY ? 1.f : fast_exp2(mc - m_new);
             mc = m_new;
-            l *= alpha;
+            l[0] *= alpha;
+            l[1] *= alpha;
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb)
                 acc[cb] *= alpha;
         }
-        const float m_p = (mc == -INFINITY ? 0.f : mc) - kShift<DT>;
-        float ps = 0.f;
+    };
+    // Sets a tile's non-finite values of V to zero (where some row does not see some key): whether there are any.
+    auto clean = [&](char *vbuf) __attribute__((always_inline)) {
+        uint32_t any = 0;
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
+        for (int j = 0; j < kPieces; ++j) {
+            const u32x4 w = *reinterpret_cast<const u32x4 *>(vbuf + (j * 256 + tid) * 16);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                s[nb][i] = fast_exp2(fmaf(s[nb][i], c, -m_p));
-                ps += s[nb][i];
-            }
-        l += ps;
-        if constexpr (kF32) {
+            for (int i = 0; i < 4; ++i)
+                any |= nonfinite<DT>(w[i]);
+        }
+        if (__syncthreads_or(any != 0) == 0)
+            return false;
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
+        for (int j = 0; j < kPieces; ++j) {
+            u32x4 w = *reinterpret_cast<const u32x4 *>(vbuf + (j * 256 + tid) * 16);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                w[i] = finite_part<DT>(w[i]);
+            *reinterpret_cast<u32x4 *>(vbuf + (j * 256 + tid) * 16) = w;
+        }
+        __syncthreads();
+        return true;
+    };
+    auto add_nonfinite = [&](int kt) __attribute__((always_inline)) {
+#pragma unroll 1
+        for (int key = kt; key <= min(kt + BN - 1, t_last); ++key) {
+            if (!sees(mask, key))
+                continue;
+            const char *v = v_base + token_offset(a, table, key);
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-#pragma unroll
-                    for (int cb = 0; cb < CB; ++cb) {
-                        const int key = nb * 32 + 8 * (i / 4) + 4 * h + i % 4;
-                        const uint32_t v = *(lds_u32 *)(vp + (v_place(key, cb * 8 + n / 4) + n % 4 * 4));
-                        acc[cb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(v), s[nb][i], acc[cb], 0, 0, 0);
-                    }
-        } else {
-            typedef typename Block<DT>::vec8 vec8;
-            typedef typename Block<DT>::type E;
-#pragma unroll
-            for (int mb = 0; mb < 2 * NB; ++mb) {
-                vec8 w[kTerms];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float left = s[mb / 2][8 * (mb & 1) + e];
-#pragma unroll
-                    for (int t = 0; t < kTerms; ++t) {
-                        w[t][e] = (E)left;
-                        left -= (float)w[t][e];
-                    }
-                }
-#pragma unroll
-                for (int cb = 0; cb < CB; ++cb) {  // sixteen keys' V^T of 32 channels: two transposed reads
-                    lds_char *const p = vp + ((v_lane ^ (cb * 64)) + 16 * mb * RB);
-                    union {
-                        s16x4 half[2];
-                        vec8 v;
-                    } r;
-                    r.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p);
-                    r.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + 8 * RB));
-#pragma unroll
-                    for (int t = 0; t < kTerms; ++t)
-                        acc[cb] = Block<DT>::mfma(r.v, w[t], acc[cb]);
-                }
-            }
-        }
-        if (partly(kt) && uniform((int)(lds_bad[buf][0] | lds_bad[buf][1] | lds_bad[buf][2] | lds_bad[buf][3])) != 0) {
-#pragma unroll 1
-            for (int key = kt; key <= min(kt + BN - 1, t_last); ++key) {
-                if (!sees(mask, key))
-                    continue;
-                const char *v = v_base + token_offset(a, table, key);
-#pragma unroll
-                for (int cb = 0; cb < CB; ++cb) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        acc[cb][i] += nonfinite_part<DT>(v, cb * 32 + 8 * (i / 4) + 4 * h + i % 4);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
+                    acc[cb][i] += nonfinite_part<DT>(v, cb * 32 + 8 * (i / 4) + 4 * h + i % 4);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
     };
 
-    if (lo < hi) {
-        int kt = lo, buf = 0;
-        if (kt >= gap_lo && kt + BN <= gap_hi)  // (a stretch can begin in the gap)
-            kt = gap_hi / BN * BN;
-        if (kt < hi) {
-            load(kt);
-            store(0, partly(kt));
+    int kt = lo, buf = 0;
+    if (kt >= gap_lo && kt + BN <= gap_hi)  // (a stretch can begin in the gap)
+        kt = gap_hi / BN * BN;
+    if (kt < hi) {
+        load(kt, 0);
+    }
+    while (kt < hi) {
+        all_loads_done();  // the wave's own ...
+        __syncthreads();   // ... and everybody's; and everybody has done with the buffers that are loaded next
+        const int following = next(kt);
+        if (following < hi) {
+            load(following, buf ^ 1);
         }
-        __syncthreads();
-        while (kt < hi) {
-            const int following = next(kt);
-            if (following < hi)
-                load(following);
-            if (kt < my_hi && kt + BN > my_lo)  // (some tiles only other waves' rows see)
-                compute(buf, kt);
-            if (following < hi)
-                store(buf ^ 1, partly(following));
-            __syncthreads();
-            buf ^= 1;
-            kt = following;
+        const bool bad = partly(kt) && clean(v_lds[buf]);
+        const char *const kb = k_lds[buf], *const vb = v_lds[buf];
+        if (kt < my_hi && kt + BN > my_lo) {  // (some tiles only other waves' rows see)
+            f32x16 s[NB];
+            // (pieces are read one ahead of their use; K's in fp32 are not: four products to a piece hide it, and the queries take 64 registers)
+            u32x4 kf[2][NB];
+            if (!kF32)
+                read_k(kb, 0, kf[0]);
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) {
+                if (kF32)
+                    read_k(kb, kk, kf[kk & 1]);
+                else if (kk + 1 < KK)
+                    read_k(kb, kk + 1, kf[(kk + 1) & 1]);
+                multiply_k(kf[kk & 1], kk, s);
+                if constexpr (kF32)
+                    __builtin_amdgcn_sched_barrier(0);
+            }
+            vpiece vf[2][CB];
+            read_v(vb, 0, vf[0]);
+            masks(s, kt, top_of(s, 0, 16 * NB, -INFINITY));
+            weigh(s, 0, 16 * NB);
+#pragma unroll
+            for (int m = 0; m < kSteps; ++m) {
+                if (m + 1 < kSteps)
+                    read_v(vb, m + 1, vf[(m + 1) & 1]);
+                multiply_v(vf[m & 1], m, s);
+                if constexpr (kF32 || MOD == kGeneral)  // (no further reads ahead: these have no registers for them)
+                    __builtin_amdgcn_sched_barrier(0);
+            }
+            if (bad)
+                add_nonfinite(kt);
         }
+        buf ^= 1;
+        kt = following;
     }
 
-    const float total = wave_xor_sum<32>(l);
+    const float total = wave_xor_sum<32>(l[0] + l[1]);
     const bool stored = wave * 32 + n < it.n_rows;
     const float inv = total == 0.f ? 0.f : 1.f / total;
-    const float lse2 = total == 0.f ? -INFINITY : (mc == -INFINITY ? 0.f : mc) + fast_log2(total) - kShift<DT>;
-    const float offset = MOD ? -mask.slope * (float)mask.dist0 : 0.f;
+    const float lse2 = total == 0.f ? -INFINITY : (mc == -INFINITY ? 0.f : mc) + fast_log2(total) - kShift<DT> + (MOD == kCapped ? a.score.cap_out : 0.f);
+    const float offset = MOD == kGeneral && a.score.slopes ? -a.score.slopes[head] * (float)mask.dist0 : 0.f;
     if (!stored)
         return;
     const int64_t at = (int64_t)(u.tok0 + token) * a.Hq + head;
@@ -380,21 +455,24 @@ __global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
     }
 }
 
-template <int DT, int D>
+template <int DT, int D, bool EXACT>
 void launch(bool modified, int64_t n_items, const TokArgs &a, hipStream_t stream)
 {
     const dim3 grid((unsigned)n_items), block(256);
-    if (DT == SPD_F32 || a.out_f32) {
-        if (modified)
-            hipLaunchKernelGGL((tokens_many_kernel<DT, D, true, true>), grid, block, 0, stream, a);
-        else
-            hipLaunchKernelGGL((tokens_many_kernel<DT, D, true, false>), grid, block, 0, stream, a);
-    } else if constexpr (DT != SPD_F32) {
-        if (modified)
-            hipLaunchKernelGGL((tokens_many_kernel<DT, D, false, true>), grid, block, 0, stream, a);
-        else
-            hipLaunchKernelGGL((tokens_many_kernel<DT, D, false, false>), grid, block, 0, stream, a);
-    }
+    if (!modified)
+        hipLaunchKernelGGL((tokens_many_kernel<DT, D, EXACT, kPlain>), grid, block, 0, stream, a);
+    else if (!EXACT && !a.score.slopes)
+        hipLaunchKernelGGL((tokens_many_kernel<DT, D, EXACT, EXACT ? kGeneral : kCapped>), grid, block, 0, stream, a);
+    else
+        hipLaunchKernelGGL((tokens_many_kernel<DT, D, EXACT, kGeneral>), grid, block, 0, stream, a);
+}
+template <int DT, int D>
+void launch(bool modified, int64_t n_items, const TokArgs &a, hipStream_t stream)
+{
+    if (DT == SPD_F32 || a.out_f32)
+        launch<DT, D, true>(modified, n_items, a, stream);
+    else if constexpr (DT != SPD_F32)
+        launch<DT, D, false>(modified, n_items, a, stream);
 }
 template <int DT>
 void launch(int head_dim, bool modified, int64_t n_items, const TokArgs &a, hipStream_t stream)

@@ -12,6 +12,7 @@
 namespace spd::host {
 
 constexpr int32_t kMaxPosition = 1 << 30;
+constexpr int64_t kMaxStrideBytes = (int64_t)1 << 28;
 
 inline bool token_stride_ok(int64_t stride, int64_t heads, int head_dim, int es)
 {
@@ -114,6 +115,9 @@ inline int validate_tokens(const spd_shape *s, const void *q, int64_t q_stride, 
         return rc;
     if (out_dtype != SPD_F32 && out_dtype != s->dtype)
         return SPD_ERR_SHAPE;
+    // the kernels' products of a token's or page's number and its stride are 32 by 32 bits
+    if (v->token_stride > kMaxStrideBytes / elt_size(s->dtype) || (v->block_size != 0 && v->block_stride > kMaxStrideBytes / elt_size(s->dtype)))
+        return SPD_ERR_ALIGN;
     if (c && (!(c->cap >= 0.f) || !std::isfinite(c->cap) || (c->causal != 0 && c->causal != 1)))
         return SPD_ERR_SHAPE;
     if (c && c->cap > 0.f && !std::isfinite(std::fabs(s->scale) / c->cap))  // (a subnormal cap)
@@ -256,10 +260,17 @@ inline int64_t stretches(const std::vector<TokTile> &tiles, int64_t chunk)
 }
 
 // The stretch length: the shortest with which all stretches run at once, but no shorter than `least` steps (each costs a partial and its join).
-// Work beyond one round of `most` steps each goes by `most`.
+// Work beyond one round goes by `most`, or whole where a tile is no more than its share of the work: splitting then only costs.
 inline int64_t stretch_steps(const std::vector<TokTile> &tiles, int64_t at_once, int64_t least, int64_t most)
 {
-    int64_t lo = least, hi = most;
+    int64_t total = 0, longest = 0;
+    for (const TokTile &t : tiles) {
+        total += t.steps;
+        longest = std::max<int64_t>(longest, t.steps);
+    }
+    if (longest <= total / at_once)
+        return std::max<int64_t>(1, longest);
+    int64_t lo = least, hi = std::max(most, total / at_once);
     if (stretches(tiles, hi) >= at_once)
         return hi;
     while (lo < hi) {
