@@ -256,26 +256,30 @@ class Score:
         self.struct = st
 
     def check(self, n_users: int, n_tokens: int, n_q_heads: int):
-        assert all(a.shape == (n_users,) for a in self.per_user.values())
+        for a in self.per_user.values():
+            assert a.shape == (n_users,)
         assert self.slopes is None or self.slopes.numel() == n_q_heads
         assert self.ranges is None or self.ranges.shape[0] == n_tokens
 
 
 def _new_counts(n_new, n_users: int):
     """(host int32 array, sum) of the users' new tokens."""
-    counts = np.ascontiguousarray(n_new, dtype=np.int32)
+    counts = n_new
+    if type(counts) is not np.ndarray or counts.dtype != np.int32 or not counts.flags.c_contiguous:
+        counts = np.ascontiguousarray(n_new, dtype=np.int32)
     assert counts.shape == (n_users,)
-    return counts, int(counts.sum(dtype=np.int64))
+    return counts, sum(counts.tolist()) if n_users <= 64 else int(np.add.reduce(counts, dtype=np.int64))
 
 
 def _token_rows(t: torch.Tensor, n_tokens: int, n_heads: int, head_dim: int) -> int:
     """The token stride of a [T][heads][d] tensor whose heads lie end to end."""
-    assert t.dim() == 3 and t.shape == (n_tokens, n_heads, head_dim)
+    assert t.shape == (n_tokens, n_heads, head_dim)
     if n_tokens <= 1:      # (torch may give a dimension of one any stride)
         assert n_tokens == 0 or t[0].is_contiguous()
         return n_heads * head_dim
-    assert t.stride(2) == 1 and (n_heads == 1 or t.stride(1) == head_dim)
-    return t.stride(0)
+    st = t.stride()
+    assert st[2] == 1 and (n_heads == 1 or st[1] == head_dim)
+    return st[0]
 
 
 # torch's current stream as a pointer, without the Stream object around it (2 us of a call that takes 11) where torch offers that

@@ -52,7 +52,8 @@ struct AppendArgs {
     const AppendItem *items;
 };
 constexpr int kTurnTokens = 4;
-constexpr int kAppendByValue = 48;  // items that travel with the arguments: a call for few users has nothing to upload
+constexpr int kAppendByValue = 16;  // items that travel with the arguments: a call for few users has nothing to upload (arguments of
+                                     // 48 items cost the host more than looking its table up: 32 users 5.0 us, 4.1 with the table)
 struct AppendItems {
     AppendItem it[kAppendByValue];
 };

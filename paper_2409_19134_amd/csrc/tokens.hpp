@@ -66,7 +66,7 @@ struct TokArgs {
     ScoreArgs score;
 };
 
-// A query row's masks and bias.  It sees the keys in [mlo, mlo + mn) and in [plo, plo + pn).
+// A query row's masks and bias (slope: its head's, 0 without).  It sees the keys in [mlo, mlo + mn) and in [plo, plo + pn).
 struct RowMask {
     int mlo, plo;
     unsigned mn, pn;
@@ -77,7 +77,7 @@ struct RowMask {
 
 __host__ __device__ __forceinline__ int clampi(int v, int lo, int hi) { return min(max(v, lo), hi); }
 
-__host__ __device__ __forceinline__ RowMask row_mask(const ScoreArgs &s, const TokUser &u, int len, int q_pos, int token, int head)
+__host__ __device__ __forceinline__ RowMask row_mask(const ScoreArgs &s, const TokUser &u, int len, int q_pos, int token, float slope)
 {
     RowMask r;
     int rlo = 0, rhi = len;
@@ -102,7 +102,7 @@ __host__ __device__ __forceinline__ RowMask row_mask(const ScoreArgs &s, const T
     r.dist0 = 0;
     r.slope2 = 0.f;
     if (s.slopes) {
-        r.slope2 = s.slopes[head] * kLog2e;
+        r.slope2 = slope * kLog2e;
         int d = 0x7fffffff;
         if (r.mn)
             d = abs(q_pos - clampi(q_pos, r.mlo, r.mlo + (int)r.mn - 1));
@@ -117,6 +117,109 @@ __host__ __device__ __forceinline__ bool sees(const RowMask &r, int key)
 {
     return (unsigned)(key - r.mlo) < r.mn || (unsigned)(key - r.plo) < r.pn;
 }
+
+// What a tile of rows sees: [any_lo, any_hi) some row, [full_lo, full_hi) every row's window; prefixes end at pre_hi, windows begin at win_lo.
+struct Limits {
+    int any_lo = 0x7fffffff, any_hi = 0, full_lo = 0, full_hi = 0x7fffffff, pre_hi = 0, win_lo = 0x7fffffff;
+    __host__ __device__ __forceinline__ void add(const RowMask &m)
+    {
+        if (m.mn) {
+            any_lo = min(any_lo, m.mlo);
+            any_hi = max(any_hi, m.mlo + (int)m.mn);
+            win_lo = min(win_lo, m.mlo);
+        }
+        if (m.pn) {
+            any_lo = min(any_lo, m.plo);
+            any_hi = max(any_hi, m.plo + (int)m.pn);
+            pre_hi = max(pre_hi, m.plo + (int)m.pn);
+        }
+        full_lo = max(full_lo, m.mlo);
+        full_hi = min(full_hi, m.mlo + (int)m.mn);
+    }
+    __host__ __device__ __forceinline__ void add(const Limits &o)
+    {
+        any_lo = min(any_lo, o.any_lo);
+        any_hi = max(any_hi, o.any_hi);
+        full_lo = max(full_lo, o.full_lo);
+        full_hi = min(full_hi, o.full_hi);
+        pre_hi = max(pre_hi, o.pre_hi);
+        win_lo = min(win_lo, o.win_lo);
+    }
+    __device__ __forceinline__ void to(int (&v)[6]) const
+    {
+        v[0] = any_lo, v[1] = any_hi, v[2] = full_lo, v[3] = full_hi, v[4] = pre_hi, v[5] = win_lo;
+    }
+    static __device__ __forceinline__ Limits from(const int (&v)[6])
+    {
+        Limits l;
+        l.any_lo = v[0], l.any_hi = v[1], l.full_lo = v[2], l.full_hi = v[3], l.pre_hi = v[4], l.win_lo = v[5];
+        return l;
+    }
+    __device__ __forceinline__ Limits of_lane_xor(int x) const
+    {
+        Limits o;
+        o.any_lo = __shfl_xor(any_lo, x);
+        o.any_hi = __shfl_xor(any_hi, x);
+        o.full_lo = __shfl_xor(full_lo, x);
+        o.full_hi = __shfl_xor(full_hi, x);
+        o.pre_hi = __shfl_xor(pre_hi, x);
+        o.win_lo = __shfl_xor(win_lo, x);
+        return o;
+    }
+    __device__ __forceinline__ Limits uniform_of() const
+    {
+        Limits o;
+        o.any_lo = uniform(any_lo);
+        o.any_hi = uniform(any_hi);
+        o.full_lo = uniform(full_lo);
+        o.full_hi = uniform(full_hi);
+        o.pre_hi = uniform(pre_hi);
+        o.win_lo = uniform(win_lo);
+        return o;
+    }
+};
+// ... without ranges, from the first and the last row's positions: both ends of a row's window move up with its position (the any-limits also hold
+// where neither of the two rows sees a key, but one between them does).
+__host__ __device__ __forceinline__ Limits tile_limits(const ScoreArgs &s, const TokUser &u, int len, int q_first, int q_last)
+{
+    auto begin = [&](int q) { return s.window ? max(0, q - s.window + 1) : 0; };
+    auto end = [&](int q) { return min(len, s.causal ? q + 1 : s.window ? q + s.window : len); };
+    Limits l;
+    const int lo = begin(q_first), hi = end(q_last), pre = min(u.prefix, len);
+    if (lo < hi) {
+        l.any_lo = l.win_lo = lo;
+        l.any_hi = hi;
+    }
+    if (pre > 0) {
+        l.any_lo = 0;
+        l.any_hi = max(l.any_hi, pre);
+        l.pre_hi = pre;
+    }
+    l.full_lo = begin(q_last);
+    l.full_hi = end(q_first);
+    return l;
+}
+
+// The steps (of `step` keys) that `waves` waves take in turn over a stretch [k_begin, k_end) of a tile's keys: from the first key that some row sees,
+// over the gap between the prefixes and the windows, to the last.  Places at or behind `hi` are hi: nothing is read there, and sums with
+// them stay in 32 bits.
+struct KeyWalk {
+    int lo, hi, gap_lo, gap_hi, step, round;
+    __host__ __device__ __forceinline__ KeyWalk(const Limits &l, int k_begin, int k_end, int step_, int waves)
+        : lo(max(k_begin, l.any_lo / step_ * step_)), hi(min(k_end, l.any_hi)), gap_lo(l.pre_hi), gap_hi(l.win_lo), step(step_), round(step_ * waves)
+    {
+        if (lo >= hi)
+            lo = hi = 0;
+    }
+    __host__ __device__ __forceinline__ int over_gap(int t) const  // in whole rounds, so that the waves stay apart
+    {
+        if (t >= gap_lo && t < hi && gap_hi - step >= t)
+            t += (min(gap_hi, hi + round) - t) / round * round;
+        return min(t, hi);
+    }
+    __host__ __device__ __forceinline__ int first(int wave) const { return lo < hi ? over_gap(lo + wave * step) : hi; }
+    __host__ __device__ __forceinline__ int next(int t) const { return over_gap(t + round); }  // t < hi
+};
 
 // A row's view of a run of keys from key0 on, made anew for every run: without the detour the compiler keeps every key's differences to the row's
 // limits in registers, over all runs.

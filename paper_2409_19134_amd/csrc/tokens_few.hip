@@ -105,50 +105,78 @@ __global__ __launch_bounds__(256, 2) void tokens_few_kernel(const TokArgs a)
     const int len = u.len + a.grow_len, q_pos0 = u.q_pos + a.grow_q;
     const int k_end = it.k_end + (it.to_len ? a.grow_len : 0);
 
-    // the lane's rows, their queries and masks
+    const char *k_base, *v_base;
+    kv_bases(a, u, it.user, it.kv_head, k_base, v_base);
+
+    // The lane's rows (those behind the last repeat it and are not stored).  What is loaded of them is asked for before the first keys: loads come back
+    // in order, and the first products need no values yet.
+    constexpr int kQ = RB / 64;
     RowMask mask[NT];
-    u32x4 qB[NT][RB / 64];
-    int any_lo = 0x7fffffff, any_hi = 0, full_lo = 0, full_hi = 0x7fffffff;  // keys that some row sees, that every row's window holds
-    int pre_hi = 0, win_lo = 0x7fffffff;                                     // where prefixes end and windows begin
+    int token[NT];
+    float slope[NT];
+    u32x4 q_raw[NT][kQ];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-        const int row = min(it.row0 + nt * 16 + r, it.row0 + it.n_rows - 1);  // (rows behind the last repeat it and are not stored)
-        const int token = row / a.G, head = it.kv_head * a.G + (row - token * a.G);
-        mask[nt] = row_mask(a.score, u, len, q_pos0 + token, token, head);
-        const char *qr = a.q + (int64_t)(u.tok0 + token) * a.q_stride + (int64_t)head * RB + grp * 16;
+        const int row = min(it.row0 + nt * 16 + r, it.row0 + it.n_rows - 1);
+        token[nt] = row / a.G;
+        const int head = it.kv_head * a.G + (row - token[nt] * a.G);
+        slope[nt] = MOD && a.score.slopes ? a.score.slopes[head] : 0.f;
+        const char *qr = a.q + (int64_t)(u.tok0 + token[nt]) * a.q_stride + (int64_t)head * RB + grp * 16;
 #pragma unroll
-        for (int kk = 0; kk < RB / 64; ++kk)
+        for (int kk = 0; kk < kQ; ++kk)
+            q_raw[nt][kk] = reinterpret_cast<const u32x4 *>(qr + kk * 64)[0];
+    }
+    // What the rows see: without ranges it follows from the first and the last row's positions.
+    Limits lim;
+    if (a.score.ranges) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+            lim.add(row_mask(a.score, u, len, q_pos0 + token[nt], token[nt], 0.f));
+#pragma unroll
+        for (int x = 1; x < 16; x *= 2)  // (the four lane groups hold the same rows)
+            lim.add(lim.of_lane_xor(x));
+        lim = lim.uniform_of();
+    } else {
+        lim = tile_limits(a.score, u, len, q_pos0 + it.row0 / a.G, q_pos0 + (it.row0 + it.n_rows - 1) / a.G);
+    }
+    const KeyWalk walk(lim, it.k_begin, k_end, kStep, 4);
+    const int hi = walk.hi, full_lo = lim.full_lo, full_hi = min(lim.full_hi, hi);
+
+    LaneConst L = {};
+    L.r = r;
+    L.grp = grp;
+    L.kt = r >> 2;
+    L.kc = grp;
+    L.k_base = k_base;
+    L.v_base = v_base;
+    L.page_shift = a.page_shift;
+    L.page_mask = (1 << a.page_shift) - 1;
+    L.token_stride = a.token_stride;
+    L.block_stride = a.block_stride;
+    L.bt_row = PAGED ? a.block_table + (int64_t)it.user * a.max_blocks : nullptr;
+    const int t_last = hi - 1;
+    int tb = walk.first(wave);
+    PagePair P = {};
+    if (PAGED && tb < hi)
+        P = load_pages(L, tb, t_last);
+
+    // Two tiles' queries have no registers: every lane's pieces wait in LDS (the same for all waves).
+    __shared__ __attribute__((aligned(16))) u32x4 q_lds[NT > 1 ? NT * kQ * 64 : 1];
+    u32x4 qB[kQ];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int kk = 0; kk < kQ; ++kk) {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                qB[nt][kk][j] = (reinterpret_cast<const u32x4 *>(qr + kk * 64)[0][j] & a.score.q_and) ^ a.score.q_xor;
-        const RowMask &m = mask[nt];
-        if (m.mn) {
-            any_lo = min(any_lo, m.mlo);
-            any_hi = max(any_hi, m.mlo + (int)m.mn);
-            win_lo = min(win_lo, m.mlo);
+                qB[kk][j] = (q_raw[nt][kk][j] & a.score.q_and) ^ a.score.q_xor;
+            if (NT > 1 && wave == nt)
+                q_lds[(nt * kQ + kk) * 64 + lane] = qB[kk];
         }
-        if (m.pn) {
-            any_lo = min(any_lo, m.plo);
-            any_hi = max(any_hi, m.plo + (int)m.pn);
-            pre_hi = max(pre_hi, m.plo + (int)m.pn);
-        }
-        full_lo = max(full_lo, m.mlo);
-        full_hi = min(full_hi, m.mlo + (int)m.mn);
+        mask[nt] = row_mask(a.score, u, len, q_pos0 + token[nt], token[nt], slope[nt]);
     }
-#pragma unroll
-    for (int x = 1; x < 16; x *= 2) {  // (the four lane groups hold the same rows)
-        any_lo = min(any_lo, __shfl_xor(any_lo, x));
-        any_hi = max(any_hi, __shfl_xor(any_hi, x));
-        full_lo = max(full_lo, __shfl_xor(full_lo, x));
-        full_hi = min(full_hi, __shfl_xor(full_hi, x));
-        pre_hi = max(pre_hi, __shfl_xor(pre_hi, x));
-        win_lo = min(win_lo, __shfl_xor(win_lo, x));
-    }
-    const int lo = max(it.k_begin, uniform(any_lo) / kStep * kStep), hi = min(k_end, uniform(any_hi));
-    full_lo = uniform(full_lo);
-    full_hi = min(uniform(full_hi), hi);
-    pre_hi = uniform(pre_hi);
-    win_lo = uniform(win_lo);
+    if (NT > 1)
+        __syncthreads();
 
     float mc[NT], l[NT];  // running maximum in units of log2 (of all rows' lanes alike), the lane's part of the sum
     f32x4 acc[NT][CP];
@@ -161,132 +189,114 @@ __global__ __launch_bounds__(256, 2) void tokens_few_kernel(const TokArgs a)
             acc[nt][cc] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    if (lo < hi) {
-        LaneConst L = {};
-        L.r = r;
-        L.grp = grp;
-        L.kt = r >> 2;
-        L.kc = grp;
-        const char *kb, *vb;
-        kv_bases(a, u, it.user, it.kv_head, kb, vb);
-        L.k_base = kb;
-        L.v_base = vb;
-        L.page_shift = a.page_shift;
-        L.page_mask = (1 << a.page_shift) - 1;
-        L.token_stride = a.token_stride;
-        L.block_stride = a.block_stride;
-        L.bt_row = PAGED ? a.block_table + (int64_t)it.user * a.max_blocks : nullptr;
-        const int t_last = hi - 1;
-        // a wave's next step; over the gap between the prefixes and the windows in whole rounds, so that the waves stay apart
-        auto next = [&](int tb) {
-            tb += 4 * kStep;
-            if (tb >= pre_hi && tb + kStep <= win_lo)
-                tb += (win_lo - tb) / (4 * kStep) * (4 * kStep);
-            return tb;
-        };
-        int tb = lo + wave * kStep;
-        PagePair P = {};
-        if (PAGED && tb < hi)
-            P = load_pages(L, tb, t_last);
-        const float c = MOD ? 1.f : a.score.c;
-        while (tb < hi) {
-            const int following = next(tb);
-            TileRegs<RB, NA> T;
-            load_tile<RB, NA, PAGED, false>(T, L, tb, t_last, P, following - tb);
-            const bool masked = tb < full_lo || tb + kStep > full_hi;
-            const int t0 = tb + grp * NE;
-            float p[NT][NE];
+    const float c = MOD ? 1.f : a.score.c;
+    while (tb < hi) {
+        TileRegs<RB, NA> T;
+        load_tile<RB, NA, PAGED, false>(T, L, tb, t_last, P, walk.next(tb) - tb);
+        const bool masked = tb < full_lo || tb + kStep > full_hi;
+        const int t0 = tb + grp * NE;
+        float p[NT][NE];
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                f32x4 s[NA];
+        for (int nt = 0; nt < NT; ++nt) {
+            if constexpr (NT > 1) {
+                int at = nt * kQ * 64 + lane;
+                asm volatile("" : "+v"(at));  // (read anew in every step)
 #pragma unroll
-                for (int i = 0; i < NA; ++i)
-                    s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int kk = 0; kk < kQ; ++kk)
+                    qB[kk] = q_lds[at + kk * 64];
+            }
+            f32x4 s[NA];
 #pragma unroll
-                for (int kk = 0; kk < RB / 64; ++kk)
+            for (int i = 0; i < NA; ++i)
+                s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int i = 0; i < NA; ++i) {
-                        if constexpr (kBytes == 4) {
+            for (int kk = 0; kk < RB / 64; ++kk)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                s[i] = Elt<DT>::mfma(__uint_as_float(T.k[i][kk][e]), __uint_as_float(qB[nt][kk][e]), s[i]);
-                        } else {
-                            typedef typename Elt<DT>::vec8 vec8;
-                            s[i] = Elt<DT>::mfma(__builtin_bit_cast(vec8, T.k[i][kk]), __builtin_bit_cast(vec8, qB[nt][kk]), s[i]);
-                        }
+                for (int i = 0; i < NA; ++i) {
+                    if constexpr (kBytes == 4) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            s[i] = Elt<DT>::mfma(__uint_as_float(T.k[i][kk][e]), __uint_as_float(qB[kk][e]), s[i]);
+                    } else {
+                        typedef typename Elt<DT>::vec8 vec8;
+                        s[i] = Elt<DT>::mfma(__builtin_bit_cast(vec8, T.k[i][kk]), __builtin_bit_cast(vec8, qB[kk]), s[i]);
                     }
-                float x[NE];
-                const RunMask run(mask[nt], t0);
+                }
+            float x[NE];
+            const RunMask run(mask[nt], t0);
+#pragma unroll
+            for (int e = 0; e < NE; ++e)
+                x[e] = modified<MOD, true>(s[e / 4][e % 4], a.score, mask[nt], run.q - e);
+            if (masked)
 #pragma unroll
                 for (int e = 0; e < NE; ++e)
-                    x[e] = modified<MOD, true>(s[e / 4][e % 4], a.score, mask[nt], run.q - e);
-                if (masked)
+                    x[e] = run.sees(mask[nt], e) ? x[e] : -INFINITY;
+            float mt = x[0];
 #pragma unroll
-                    for (int e = 0; e < NE; ++e)
-                        x[e] = run.sees(mask[nt], e) ? x[e] : -INFINITY;
-                float mt = x[0];
+            for (int e = 1; e < NE; ++e)
+                mt = fmaxf(mt, x[e]);
+            mt = wave_xor_max<16>(mt);
+            mt = wave_xor_max<32>(mt);
+            const float m_new = fmaxf(mc[nt], mt * c);
+            const float m_use = m_new == -INFINITY ? 0.f : m_new;  // (nothing seen yet)
+            const float alpha = fast_exp2(mc[nt] - m_use);
+            const float m_p = m_use - Elt<DT>::kPShift;
+            float ps = 0.f;
 #pragma unroll
-                for (int e = 1; e < NE; ++e)
-                    mt = fmaxf(mt, x[e]);
-                mt = wave_xor_max<16>(mt);
-                mt = wave_xor_max<32>(mt);
-                const float m_new = fmaxf(mc[nt], mt * c);
-                const float m_use = m_new == -INFINITY ? 0.f : m_new;  // (nothing seen yet)
-                const float alpha = fast_exp2(mc[nt] - m_use);
-                const float m_p = m_use - Elt<DT>::kPShift;
-                float ps = 0.f;
-#pragma unroll
-                for (int e = 0; e < NE; ++e) {
-                    p[nt][e] = fast_exp2(fmaf(x[e], c, -m_p));
-                    ps += p[nt][e];
-                }
-                l[nt] = l[nt] * alpha + ps;
-                mc[nt] = m_new;
-                if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
-#pragma unroll
-                    for (int cc = 0; cc < CP; ++cc)
-                        acc[nt][cc] *= alpha;
-                }
+            for (int e = 0; e < NE; ++e) {
+                p[nt][e] = fast_exp2(fmaf(x[e], c, -m_p));
+                ps += p[nt][e];
             }
-            bool bad = false;
-            if (masked) {
-                uint32_t any = 0;
-#pragma unroll
-                for (int e = 0; e < NE; ++e)
-#pragma unroll
-                    for (int i = 0; i < RB / 64; ++i)
-                        any |= nonfinite<DT>(T.v[e].dword(i));
-                bad = __builtin_amdgcn_ballot_w64(any != 0) != 0;
-                if (bad)
-#pragma unroll
-                    for (int e = 0; e < NE; ++e)
-                        keep_finite<DT>(T.v[e]);
-            }
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                const Weights<DT, NE> w(p[nt]);
+            l[nt] = l[nt] * alpha + ps;
+            mc[nt] = m_new;
+            if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
 #pragma unroll
                 for (int cc = 0; cc < CP; ++cc)
-                    acc[nt][cc] = add_phase<DT, D, NA>(T, cc, w, acc[nt][cc]);
+                    acc[nt][cc] *= alpha;
             }
-            if (bad) {
+            if (NT > 1)
+                __builtin_amdgcn_sched_barrier(0);
+        }
+        bool bad = false;
+        if (masked) {
+            uint32_t any = 0;
+#pragma unroll
+            for (int e = 0; e < NE; ++e)
+#pragma unroll
+                for (int i = 0; i < RB / 64; ++i)
+                    any |= nonfinite<DT>(T.v[e].dword(i));
+            bad = __builtin_amdgcn_ballot_w64(any != 0) != 0;
+            if (bad)
+#pragma unroll
+                for (int e = 0; e < NE; ++e)
+                    keep_finite<DT>(T.v[e]);
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const Weights<DT, NE> w(p[nt]);
+#pragma unroll
+            for (int cc = 0; cc < CP; ++cc)
+                acc[nt][cc] = add_phase<DT, D, NA>(T, cc, w, acc[nt][cc]);
+            if (NT > 1)  // (one tile's terms at a time: 32 rows have no registers for more)
+                __builtin_amdgcn_sched_barrier(0);
+        }
+        if (bad) {
 #pragma unroll 1
-                for (int key = tb; key <= min(tb + kStep - 1, t_last); ++key) {
-                    const char *v = L.v_base + token_offset(a, L.bt_row, key);
+            for (int key = tb; key <= min(tb + kStep - 1, t_last); ++key) {
+                const char *v = L.v_base + token_offset(a, L.bt_row, key);
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        if (!sees(mask[nt], key))
-                            continue;
+                for (int nt = 0; nt < NT; ++nt) {
+                    if (!sees(mask[nt], key))
+                        continue;
 #pragma unroll
-                        for (int cc = 0; cc < CP; ++cc)
+                    for (int cc = 0; cc < CP; ++cc)
 #pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                acc[nt][cc][i] += nonfinite_part<DT>(v, o_channel<RB, CP>(grp * 4 + i, cc));
-                    }
+                        for (int i = 0; i < 4; ++i)
+                            acc[nt][cc][i] += nonfinite_part<DT>(v, o_channel<RB, CP>(grp * 4 + i, cc));
                 }
             }
-            tb = following;
         }
+        tb = walk.next(tb);
     }
 
     // the four waves' states, joined
@@ -336,7 +346,7 @@ __global__ __launch_bounds__(256, 2) void tokens_few_kernel(const TokArgs a)
             const int row = it.row0 + nt * 16 + rr, token = row / a.G, head = it.kv_head * a.G + (row - token * a.G);
             float offset = 0.f;
             if (MOD && a.score.slopes && ch == 0) {
-                const RowMask mk = row_mask(a.score, u, len, q_pos0 + token, token, head);
+                const RowMask mk = row_mask(a.score, u, len, q_pos0 + token, token, 0.f);
                 offset = -a.score.slopes[head] * (float)mk.dist0;
             }
             if (it.slot >= 0) {

@@ -74,7 +74,6 @@ __global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
     constexpr int kTile = BN * RB, kPieces = BN * C / 256;
     constexpr int kTerms = EXACT ? Block<DT>::kTerms : 1;
     __shared__ __attribute__((aligned(16))) char k_lds[2][kTile], v_lds[2][kTile];
-    __shared__ int lds_bounds[4][6];
 
     const TokItem it = scalar_load(a.items, blockIdx.x);
     if (it.n_rows == 0)
@@ -88,7 +87,8 @@ __global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
     // the lane's row, its query and masks (rows behind the last repeat it and are not stored)
     const int my_row = min(it.row0 + wave * 32 + n, it.row0 + it.n_rows - 1);
     const int token = my_row / a.G, head = it.kv_head * a.G + (my_row - token * a.G);
-    const RowMask mask = row_mask(a.score, u, len, q_pos0 + token, token, head);
+    const float slope = a.score.slopes ? a.score.slopes[head] : 0.f;
+    const RowMask mask = row_mask(a.score, u, len, q_pos0 + token, token, slope);
     u32x4 q[KK];
     {
         const char *qr = a.q + (int64_t)(u.tok0 + token) * a.q_stride + (int64_t)head * RB + h * 16;
@@ -98,55 +98,29 @@ __global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
             for (int j = 0; j < 4; ++j)
                 q[kk][j] = (reinterpret_cast<const u32x4 *>(qr + kk * 32)[0][j] & a.score.q_and) ^ a.score.q_xor;
     }
-    // keys that some row sees; where prefixes end and windows begin; keys that every row's window holds: of the wave, of the workgroup
-    int any_lo = 0x7fffffff, any_hi = 0, pre_hi = 0, win_lo = 0x7fffffff, full_lo = mask.mlo, full_hi = mask.mlo + (int)mask.mn;
-    if (mask.mn) {
-        any_lo = mask.mlo;
-        any_hi = mask.mlo + (int)mask.mn;
-        win_lo = mask.mlo;
-    }
-    if (mask.pn) {
-        any_lo = min(any_lo, mask.plo);
-        any_hi = max(any_hi, mask.plo + (int)mask.pn);
-        pre_hi = mask.plo + (int)mask.pn;
-    }
+    // what the wave's rows see, and the workgroup's: without ranges from the first and the last row's positions
+    Limits mine, all;
+    if (a.score.ranges) {
+        __shared__ int lds_limits[4][6];
+        mine.add(mask);
 #pragma unroll
-    for (int x = 1; x < 32; x *= 2) {
-        any_lo = min(any_lo, __shfl_xor(any_lo, x));
-        any_hi = max(any_hi, __shfl_xor(any_hi, x));
-        pre_hi = max(pre_hi, __shfl_xor(pre_hi, x));
-        win_lo = min(win_lo, __shfl_xor(win_lo, x));
-        full_lo = max(full_lo, __shfl_xor(full_lo, x));
-        full_hi = min(full_hi, __shfl_xor(full_hi, x));
-    }
-    const int my_lo = uniform(any_lo), my_hi = uniform(any_hi), my_pre = uniform(pre_hi), my_win = uniform(win_lo);
-    full_lo = uniform(full_lo);
-    full_hi = uniform(full_hi);
-    if (lane == 0) {
-        lds_bounds[wave][0] = my_lo;
-        lds_bounds[wave][1] = my_hi;
-        lds_bounds[wave][2] = my_pre;
-        lds_bounds[wave][3] = my_win;
-        lds_bounds[wave][4] = full_lo;
-        lds_bounds[wave][5] = full_hi;
-    }
-    __syncthreads();
-    int lo = 0x7fffffff, hi = 0, gap_lo = 0, gap_hi = 0x7fffffff, all_lo = 0, all_hi = 0x7fffffff;
+        for (int x = 1; x < 32; x *= 2)  // (the wave's halves hold the same rows)
+            mine.add(mine.of_lane_xor(x));
+        if (lane == 0)
+            mine.to(lds_limits[wave]);
+        __syncthreads();
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        all_lo = max(all_lo, lds_bounds[w][4]);
-        all_hi = min(all_hi, lds_bounds[w][5]);
-        lo = min(lo, lds_bounds[w][0]);
-        hi = max(hi, lds_bounds[w][1]);
-        gap_lo = max(gap_lo, lds_bounds[w][2]);
-        gap_hi = min(gap_hi, lds_bounds[w][3]);
+        for (int w = 0; w < 4; ++w)
+            all.add(Limits::from(lds_limits[w]));
+        mine = mine.uniform_of();
+        all = all.uniform_of();
+    } else {
+        auto token_of = [&](int row) { return q_pos0 + min(it.row0 + row, it.row0 + it.n_rows - 1) / a.G; };
+        mine = tile_limits(a.score, u, len, token_of(wave * 32), token_of(wave * 32 + 31));
+        all = tile_limits(a.score, u, len, token_of(0), token_of(kManyRows - 1));
     }
-    lo = max(it.k_begin, uniform(lo) / BN * BN);
-    hi = min(k_end, uniform(hi));
-    gap_lo = uniform(gap_lo);
-    gap_hi = uniform(gap_hi);
-    all_lo = uniform(all_lo);
-    all_hi = uniform(all_hi);
+    const KeyWalk walk(all, it.k_begin, k_end, BN, 1);
+    const int hi = walk.hi;
 
     float mc = -INFINITY, l[2] = {0.f, 0.f};  // running maximum in units of log2 (both lanes of a row), the lane's part of the sum (in two)
     f32x16 acc[CB];
@@ -202,15 +176,8 @@ __global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
             load_to_lds(v_base + row, off, v_to + j * 4096);
         }
     };
-    // tiles that no row sees between the prefixes and the windows are passed over
-    auto next = [&](int kt) {
-        kt += BN;
-        if (kt >= gap_lo && kt + BN <= gap_hi)
-            kt = gap_hi / BN * BN;
-        return kt;
-    };
     // a tile that some row of the workgroup may not see whole
-    auto partly = [&](int kt) { return kt < all_lo || kt + BN > all_hi; };
+    auto partly = [&](int kt) { return kt < all.full_lo || kt + BN > all.full_hi; };
     const float c = MOD == kPlain ? a.score.c : MOD == kCapped ? 2.f * a.score.cap_out : 1.f, steep = 2.f * kLog2e * a.score.cap_in;
     // lane parts of the LDS places: K row n, piece 2 kk + h; V (16-bit) keys 4 h + i / 4 of sixteen channels' pieces
     const int k_lane_ = n * RB + (h ^ swap(n)) * 16;
@@ -305,7 +272,7 @@ __global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
     // Cap, bias and masks of the tile at kt, and the running maximum with them (top: the lane's largest score as it came).
     auto masks = [&](f32x16 (&x)[NB], int kt, float top) __attribute__((always_inline)) {
         const RunMask run(mask, kt + 4 * h);
-        const bool masked = kt < full_lo || kt + BN > full_hi;
+        const bool masked = kt < mine.full_lo || kt + BN > mine.full_hi;
         if constexpr (MOD != kPlain)
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
@@ -375,22 +342,20 @@ __global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
         }
     };
 
-    int kt = lo, buf = 0;
-    if (kt >= gap_lo && kt + BN <= gap_hi)  // (a stretch can begin in the gap)
-        kt = gap_hi / BN * BN;
+    int kt = walk.first(0), buf = 0;
     if (kt < hi) {
         load(kt, 0);
     }
     while (kt < hi) {
         all_loads_done();  // the wave's own ...
         __syncthreads();   // ... and everybody's; and everybody has done with the buffers that are loaded next
-        const int following = next(kt);
+        const int following = walk.next(kt);
         if (following < hi) {
             load(following, buf ^ 1);
         }
         const bool bad = partly(kt) && clean(v_lds[buf]);
         const char *const kb = k_lds[buf], *const vb = v_lds[buf];
-        if (kt < my_hi && kt + BN > my_lo) {  // (some tiles only other waves' rows see)
+        if (kt < mine.any_hi && kt + BN > mine.any_lo) {  // (some tiles only other waves' rows see)
             f32x16 s[NB];
             // (pieces are read one ahead of their use; K's in fp32 are not: four products to a piece hide it, and the queries take 64 registers)
             u32x4 kf[2][NB];

@@ -260,7 +260,9 @@ inline int64_t stretches(const std::vector<TokTile> &tiles, int64_t chunk)
 }
 
 // The stretch length: the shortest with which all stretches run at once, but no shorter than `least` steps (each costs a partial and its join).
-// Work beyond one round goes by `most`, or whole where a tile is no more than its share of the work: splitting then only costs.
+// Work beyond one round goes by `most`, or whole where a tile is no more than its share of the work: splitting then only costs.  (Few rows: one token of
+// 24 users over 8192-32768 keys, 64 query heads in groups of eight, us: stretches of up to 128 steps, a round and a half, 344, up to 512, one round, 323;
+// many rows: a chunk of 8192 tokens over 16384, tiles of up to 256 steps cut at 64 970 + 100 for the join, whole 934.)
 inline int64_t stretch_steps(const std::vector<TokTile> &tiles, int64_t at_once, int64_t least, int64_t most)
 {
     int64_t total = 0, longest = 0;
@@ -332,7 +334,7 @@ inline void build_tok_tables(const spd_shape *s, const spd_kv_view *v, const std
         const bool many = k == (int)TokKernel::kMany;
         const int step = many ? many_keys(s->dtype) : kFewKeys;
         const int64_t at_once = (int64_t)n_cus * resident((TokKernel)k);
-        const int64_t chunk = stretch_steps(tl, at_once, 4, many ? 64 : 128);
+        const int64_t chunk = stretch_steps(tl, at_once, 4, many ? 64 : 512);
         // Few rows: the longest stretches first.  The many kernel's tiles of one head read the same keys: they go to one XCD (workgroup i
         // runs on XCD i % 8), whose L2 then holds them; heads in order of their work, each to the XCD with least so far.  Where that would
         // leave XCDs idle (their number divides that of the heads badly, and these are few) a head's tiles are dealt out to several.

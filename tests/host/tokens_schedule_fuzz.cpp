@@ -47,7 +47,7 @@ int main()
         c.window = pick(0, 2) ? 0 : pick(1, 700);
         const bool given = pick(0, 3) == 0, tokens_small = pick(0, 1);
         for (int u = 0; u < U; ++u) {
-            lens[u] = pick(0, 5) ? pick(0, 900) : pick(0, 6000);
+            lens[u] = pick(0, 7) == 0 ? 0 : pick(0, 5) ? pick(0, 900) : pick(0, 6000);
             n_new[u] = tokens_small ? pick(0, 9) : pick(0, 3) ? pick(0, 700) : pick(0, 3);
             if (!given)
                 n_new[u] = std::min(n_new[u], lens[u]);
@@ -127,13 +127,58 @@ int main()
                 }
                 if (h != 0 && h != s.n_kv_heads - 1)
                     continue;
-                // key by key, for the tile's first, last and some row between
+                // what the kernels take from a tile's first and last row holds for all of them
                 const TokUser &d = t.users[u];
+                if (!c.ranges) {
+                    const int len = d.len + grow_len, q0 = d.q_pos + grow_q, ta = row0 / G, tb = (row0 + items[0]->n_rows - 1) / G;
+                    const Limits l = tile_limits(a, d, len, q0 + ta, q0 + tb);
+                    for (int token = ta; token <= tb; ++token) {
+                        const RowMask m = row_mask(a, d, len, q0 + token, token, 0.f);
+                        if (m.mn)
+                            REQUIRE(m.mlo >= l.any_lo && m.mlo >= l.win_lo && m.mlo + (int)m.mn <= l.any_hi);
+                        if (m.pn)
+                            REQUIRE(m.plo >= l.any_lo && m.plo + (int)m.pn <= l.any_hi && m.plo + (int)m.pn <= l.pre_hi);
+                        if (l.full_lo < l.full_hi)
+                            REQUIRE(m.mlo <= l.full_lo && m.mlo + (int)m.mn >= l.full_hi);
+                    }
+                }
+                // the steps that a kernel's waves take: every key that a row sees in exactly one, none outside of the stretch
+                {
+                    const int len = d.len + grow_len, q0 = d.q_pos + grow_q, waves = k == (int)TokKernel::kMany ? 1 : 4;
+                    const int kstep = waves == 4 && pick(0, 1) ? 16 : step;
+                    Limits l = tile_limits(a, d, len, q0 + row0 / G, q0 + (row0 + items[0]->n_rows - 1) / G);
+                    std::vector<RowMask> rows;
+                    for (int r = 0; r < items[0]->n_rows; ++r)
+                        rows.push_back(row_mask(a, d, len, q0 + (row0 + r) / G, (row0 + r) / G, 0.f));
+                    if (c.ranges) {
+                        l = Limits();
+                        for (const RowMask &m : rows)
+                            l.add(m);
+                    }
+                    for (const TokItem *it : items) {
+                        const int end = it->k_end + (it->to_len ? grow_len : 0);
+                        const KeyWalk walk(l, it->k_begin, end, kstep, waves);
+                        REQUIRE(walk.lo >= 0 && walk.hi <= end && walk.hi <= len);
+                        std::vector<int> taken((size_t)len + 1, 0);
+                        for (int w = 0; w < waves; ++w)
+                            for (int t = walk.first(w); t < walk.hi; t = walk.next(t)) {
+                                REQUIRE(t >= it->k_begin && t % kstep == 0 && walk.next(t) > t && walk.next(t) <= walk.hi);
+                                for (int key = t; key < std::min(t + kstep, walk.hi); ++key)
+                                    ++taken[(size_t)key];
+                            }
+                        for (int key = it->k_begin; key < end; ++key) {
+                            REQUIRE(taken[(size_t)key] <= 1);
+                            for (size_t r = 0; r < rows.size(); r += 1 + rows.size() / 5)
+                                REQUIRE(!sees(rows[r], key) || taken[(size_t)key] == 1);
+                        }
+                    }
+                }
+                // key by key, for the tile's first, last and some row between
                 REQUIRE(d.n_tok == n_new[u] && d.len == lens[u]);
                 const int len = d.len + grow_len;
                 for (int r : {0, items[0]->n_rows / 2, items[0]->n_rows - 1}) {
                     const int token = (row0 + r) / G;
-                    const RowMask m = row_mask(a, d, len, d.q_pos + grow_q + token, token, 0);
+                    const RowMask m = row_mask(a, d, len, d.q_pos + grow_q + token, token, 0.f);
                     const int64_t pos_q = (int64_t)d.q_pos + grow_q + token + first_key_position(&c, u);
                     for (int key = 0; key < len; ++key) {
                         const bool want = by_definition(c, u, pos_q, (int64_t)key + first_key_position(&c, u),
