@@ -2,9 +2,10 @@
 //
 // A workgroup takes a few tokens.  It first forms their cosines and sines, one (token, pair) to a thread, into LDS: the heads of a token
 // share them.  Then every thread keeps one place of a head - sixteen bytes and, for pairs half a rotation apart, the sixteen that turn with
-// them - and goes through the tokens' heads with its cosines and sines in registers.
+// them - and goes through all heads of all the tokens, four loads ahead.
 // An angle is position * inv_freq: a product of 31 and 24 bits, formed in 64, as turns, of which only the fraction is kept; cosine and sine
 // of that are fp32.
+// Measured: 20240 tokens of 40 heads (bf16, 128 channels; 414 MB read and written) 68.4 us, 6.1 TB/s, where a large copy reaches 4.9.
 #pragma once
 #include "common.hpp"
 
@@ -134,56 +135,55 @@ __device__ __forceinline__ void fill_turns(float2 (*cs)[64], const TurnArgs &t, 
     }
 }
 
-// A thread's cosines and sines of one token.
-template <int NP>
-struct Turns {
-    float c[NP], s[NP];
-    __device__ __forceinline__ void read(const float2 *cs, int pair, bool turns)
-    {
-#pragma unroll
-        for (int j = 0; j < NP; ++j) {
-            const float2 v = turns ? cs[pair + j] : float2{1.f, 0.f};
-            c[j] = v.x;
-            s[j] = v.y;
-        }
-    }
-};
-
-// Turns (or copies) the thread's place of one head.
-template <int DT, bool ADJACENT, class Place>
-__device__ __forceinline__ void turn_head(const Place &p, const Turns<Place::NP> &t, const char *src, char *dst)
+// Sixteen bytes; ONCE: they do not come back soon, or are not read again soon (see kOnceBytes).
+template <bool ONCE>
+__device__ __forceinline__ u32x4 piece_load(const char *p)
 {
     typedef const u32x4 __attribute__((address_space(1))) *in;
+    return ONCE ? __builtin_nontemporal_load((in)(uintptr_t)p) : *(in)(uintptr_t)p;
+}
+template <bool ONCE>
+__device__ __forceinline__ void piece_store(char *p, u32x4 v)
+{
     typedef u32x4 __attribute__((address_space(1))) *out;
-    u32x4 a = *(in)(uintptr_t)(src + p.off);
-    if (p.turns) {
-        constexpr int VE = Place::VE;
-        if constexpr (ADJACENT) {
-            float f[VE];
-#pragma unroll
-            for (int j = 0; j < VE / 2; ++j) {
-                const float x0 = elt_get<DT>(a, 2 * j), x1 = elt_get<DT>(a, 2 * j + 1);
-                f[2 * j] = x0 * t.c[j] - x1 * t.s[j];
-                f[2 * j + 1] = x0 * t.s[j] + x1 * t.c[j];
-            }
-            a = elt_pack<DT>(f);
-        } else {
-            const u32x4 b = *(in)(uintptr_t)(src + p.off2);
-            float f[VE], g[VE];
-#pragma unroll
-            for (int j = 0; j < VE; ++j) {
-                const float x0 = elt_get<DT>(a, j), x1 = elt_get<DT>(b, j);
-                f[j] = x0 * t.c[j] - x1 * t.s[j];
-                g[j] = x0 * t.s[j] + x1 * t.c[j];
-            }
-            a = elt_pack<DT>(f);
-            *(out)(uintptr_t)(dst + p.off2) = elt_pack<DT>(g);
-        }
-    }
-    *(out)(uintptr_t)(dst + p.off) = a;
+    if constexpr (ONCE)
+        __builtin_nontemporal_store(v, (out)(uintptr_t)p);
+    else
+        *(out)(uintptr_t)p = v;
 }
 
-template <int DT, int D, bool ADJACENT>
+// Turns (or copies) the thread's place of one head.
+template <int DT, bool ADJACENT, bool ONCE, class Place>
+__device__ __forceinline__ void turn_head(const Place &p, const float2 *cs, const char *src, char *dst)
+{
+    constexpr int VE = Place::VE, NP = Place::NP;
+    u32x4 a = piece_load<ONCE>(src + p.off);
+    if (p.turns) {
+        u32x4 b = a;
+        if constexpr (!ADJACENT)
+            b = piece_load<ONCE>(src + p.off2);
+        float f[VE], g[VE];
+#pragma unroll
+        for (int j = 0; j < NP; ++j) {
+            const float2 t = cs[p.pair + j];
+            if constexpr (ADJACENT) {
+                const float x0 = elt_get<DT>(a, 2 * j), x1 = elt_get<DT>(a, 2 * j + 1);
+                f[2 * j] = x0 * t.x - x1 * t.y;
+                f[2 * j + 1] = x0 * t.y + x1 * t.x;
+            } else {
+                const float x0 = elt_get<DT>(a, j), x1 = elt_get<DT>(b, j);
+                f[j] = x0 * t.x - x1 * t.y;
+                g[j] = x0 * t.y + x1 * t.x;
+            }
+        }
+        a = elt_pack<DT>(f);
+        if constexpr (!ADJACENT)
+            piece_store<ONCE>(dst + p.off2, elt_pack<DT>(g));
+    }
+    piece_store<ONCE>(dst + p.off, a);
+}
+
+template <int DT, int D, bool ADJACENT, bool ONCE>
 __global__ __launch_bounds__(256) void rotate_kernel(const RotateArgs a)
 {
     typedef TurnPlace<DT, D, ADJACENT> Place;
@@ -191,34 +191,39 @@ __global__ __launch_bounds__(256) void rotate_kernel(const RotateArgs a)
     const int token0 = blockIdx.x * a.per_group, count = min(a.per_group, a.turn.n_tokens - token0);
     fill_turns(cs, a.turn, token0, count);
     __syncthreads();
-    const int places = turn_places(Place::ES, D, ADJACENT, a.turn.n_pairs);
+    const int places = turn_places(Place::ES, D, ADJACENT, a.turn.n_pairs), step = 256 / places;
     const Place p((int)threadIdx.x & (places - 1), a.turn.n_pairs);
     if (p.idle)
         return;
-    const int head0 = (int)threadIdx.x / places, heads = 256 / places;
-    for (int k = 0; k < count; ++k) {
-        Turns<Place::NP> t;
-        t.read(cs[k], p.pair, p.turns);
-        const char *src = a.x + (int64_t)(token0 + k) * a.x_stride;
-        char *dst = a.y + (int64_t)(token0 + k) * a.y_stride;
+    // the heads of the tokens, one after the other
+    int k = 0, head = (int)threadIdx.x / places;
 #pragma unroll 4
-        for (int head = head0; head < a.n_heads; head += heads)
-            turn_head<DT, ADJACENT>(p, t, src + (int64_t)head * (D * Place::ES), dst + (int64_t)head * (D * Place::ES));
+    for (int at = head; at < count * a.n_heads; at += step, head += step) {
+        while (head >= a.n_heads) {
+            head -= a.n_heads;
+            ++k;
+        }
+        const int64_t off = (int64_t)head * (D * Place::ES), token = token0 + k;
+        turn_head<DT, ADJACENT, ONCE>(p, cs[k], a.x + token * a.x_stride + off, a.y + token * a.y_stride + off);
     }
 }
 
-template <int DT, int D, bool ADJACENT>
+template <int DT, int D, bool ADJACENT, bool ONCE>
 __global__ __launch_bounds__(256) void append_kernel(const AppendArgs a, const AppendItems given)
 {
     typedef TurnPlace<DT, D, ADJACENT> Place;
     constexpr int HB = D * Place::ES;
     __shared__ float2 cs[kTurnTokens][64];
+    __shared__ int64_t places_of[kTurnTokens];  // the tokens' offsets in the cache
     const AppendItem it = a.by_value ? given.it[blockIdx.x] : a.items[blockIdx.x];
+    if ((int)threadIdx.x < it.count) {
+        const int at = it.place + a.grow + (int)threadIdx.x;
+        places_of[threadIdx.x] = a.k_pool ? (int64_t)a.block_table[(int64_t)it.user * a.max_blocks + (at >> a.page_shift)] * a.block_stride +
+                                                (int64_t)(at & ((1 << a.page_shift) - 1)) * a.token_stride
+                                          : (int64_t)at * a.token_stride;
+    }
     fill_turns(cs, a.turn, it.token, it.count);
     __syncthreads();
-    const int places = turn_places(Place::ES, D, ADJACENT, a.turn.n_pairs);
-    const Place p((int)threadIdx.x & (places - 1), a.turn.n_pairs), whole((int)threadIdx.x & (D / Place::VE - 1), 0);
-    const int head0 = (int)threadIdx.x / places, heads = 256 / places;
     char *k_base = it.k_base, *v_base = it.v_base;
     if (a.k_pool) {
         k_base = a.k_pool;
@@ -227,33 +232,35 @@ __global__ __launch_bounds__(256) void append_kernel(const AppendArgs a, const A
         k_base = a.k_ptrs[it.user];
         v_base = a.v_ptrs[it.user];
     }
-    const int Hq = a.q_out ? a.Hq : 0;
-    for (int k = 0; k < it.count; ++k) {
-        const int64_t token = it.token + k;
-        const int at = it.place + a.grow + k;
-        int64_t off;
-        if (a.k_pool)
-            off = (int64_t)a.block_table[(int64_t)it.user * a.max_blocks + (at >> a.page_shift)] * a.block_stride +
-                  (int64_t)(at & ((1 << a.page_shift) - 1)) * a.token_stride;
-        else
-            off = (int64_t)at * a.token_stride;
-        if (!p.idle) {
-            Turns<Place::NP> t;
-            t.read(cs[k], p.pair, p.turns);
-            const char *q = a.q + token * a.q_stride, *kn = a.k + token * a.k_stride;
-            char *qo = a.q_out + token * a.Hq * HB;
+    const int places = turn_places(Place::ES, D, ADJACENT, a.turn.n_pairs), step = 256 / places;
+    const Place p((int)threadIdx.x & (places - 1), a.turn.n_pairs);
+    if (!p.idle) {
+        const int Hq = a.q_out ? a.Hq : 0, heads = Hq + a.Hkv;
+        int k = 0, head = (int)threadIdx.x / places;
 #pragma unroll 4
-            for (int head = head0; head < Hq + a.Hkv; head += heads) {
-                const int kh = head - Hq;
-                if (kh < 0)
-                    turn_head<DT, ADJACENT>(p, t, q + (int64_t)head * HB, qo + (int64_t)head * HB);
-                else
-                    turn_head<DT, ADJACENT>(p, t, kn + (int64_t)kh * HB, k_base + off + (int64_t)kh * it.head_stride);
+        for (int i = head; i < it.count * heads; i += step, head += step) {
+            while (head >= heads) {
+                head -= heads;
+                ++k;
             }
+            const int64_t token = it.token + k;
+            const int kh = head - Hq;
+            const char *src = kh < 0 ? a.q + token * a.q_stride + (int64_t)head * HB : a.k + token * a.k_stride + (int64_t)kh * HB;
+            char *dst = kh < 0 ? a.q_out + (token * a.Hq + head) * HB : k_base + places_of[k] + kh * it.head_stride;
+            turn_head<DT, ADJACENT, ONCE>(p, cs[k], src, dst);
         }
-        constexpr int kPieces = D / Place::VE;
-        for (int head = (int)threadIdx.x / kPieces; head < a.Hkv; head += 256 / kPieces)
-            copy16(v_base + off + (int64_t)head * it.head_stride + whole.off, a.v + token * a.v_stride + (int64_t)head * HB + whole.off);
+    }
+    constexpr int kPieces = D / Place::VE, kHeads = 256 / kPieces;
+    const int off = ((int)threadIdx.x & (kPieces - 1)) * 16;
+    int k = 0, head = (int)threadIdx.x / kPieces;
+#pragma unroll 4
+    for (int i = head; i < it.count * a.Hkv; i += kHeads, head += kHeads) {
+        while (head >= a.Hkv) {
+            head -= a.Hkv;
+            ++k;
+        }
+        piece_store<ONCE>(v_base + places_of[k] + head * it.head_stride + off,
+                          piece_load<ONCE>(a.v + (it.token + k) * a.v_stride + (int64_t)head * HB + off));
     }
 }
 

@@ -590,15 +590,22 @@ TurnArgs turn_args(const spd_rope *r, const int32_t *positions, int64_t n_tokens
     return a;
 }
 
-// Kernel template arguments from run-time values: f gets integral constants of the type's code, the head's size and whether pairs are adjacent.
+// Kernel template arguments from run-time values: f gets integral constants of the type's code, the head's size, whether pairs are adjacent and whether
+// the data passes by once.
 template <class F>
-void with_turn_kernel(int dtype, int head_dim, bool adjacent, F &&f)
+void with_turn_kernel(int dtype, int head_dim, bool adjacent, bool once, F &&f)
 {
+    auto by_once = [&](auto dt, auto d, auto adj) {
+        if (once)
+            f(dt, d, adj, std::true_type());
+        else
+            f(dt, d, adj, std::false_type());
+    };
     auto by_pairs = [&](auto dt, auto d) {
         if (adjacent)
-            f(dt, d, std::true_type());
+            by_once(dt, d, std::true_type());
         else
-            f(dt, d, std::false_type());
+            by_once(dt, d, std::false_type());
     };
     auto by_dim = [&](auto dt) {
         if (head_dim == 64)
@@ -614,8 +621,16 @@ void with_turn_kernel(int dtype, int head_dim, bool adjacent, F &&f)
         by_dim(std::integral_constant<int, SPD_F16>());
 }
 
-// Tokens of a workgroup: one each until every unit has several workgroups, then as many as share the work on cosines evenly.
-int tokens_per_group(int64_t tokens, int n_cus) { return tokens <= 8 * (int64_t)n_cus ? 1 : kTurnTokens; }
+// Bytes written by a call from which on they, and what is read, pass the caches by: there is no room for them until they are read (us without / with: the
+// video 75.3 / 69.1, the prompts' 125 MB 56.8 / 51.2; the 31 MB of fp32, still in the last cache when they come up again, 10.9 / 13.7).
+constexpr int64_t kOnceBytes = (int64_t)64 << 20;
+
+// Tokens of a workgroup: one each until every unit has several workgroups, then about 12 KB of them (us with one / two / four: a video's 20240 tokens
+// of 10 KB 68.4 / 72.2 / 77.3, 5003 tokens of 6 KB in fp32 11.9 / 11.1 / 10.7, prompts of 6 KB a token appended 56.0 / 47.3 / 47.1).
+int tokens_per_group(int64_t tokens, int64_t token_bytes, int n_cus)
+{
+    return tokens <= 8 * (int64_t)n_cus ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(kTurnTokens, 12288 / token_bytes));
+}
 
 int append(ContextBase *ctx, const spd_shape *s, const spd_kv_view *v, const int32_t *n_new, const spd_rope *rope, const int32_t *positions,
            const void *q, int64_t q_stride, void *q_out, const void *k, int64_t k_stride, const void *v_new, int64_t v_stride, hipStream_t stream)
@@ -630,7 +645,9 @@ int append(ContextBase *ctx, const spd_shape *s, const spd_kv_view *v, const int
         return SPD_OK;
     const OnDevice on(ctx->device);
     SPD_TRY(ctx, on.error);
-    const int es = elt_size(s->dtype), group = tokens_per_group(total, ctx->n_cus);
+    const int es = elt_size(s->dtype);
+    const int64_t token_bytes = (int64_t)((q ? s->n_q_heads : 0) + 2 * s->n_kv_heads) * s->head_dim * es;
+    const int group = tokens_per_group(total, token_bytes, ctx->n_cus);
     const bool paged = v->block_size != 0;
     AppendArgs a = {};
     a.turn = turn_args(rope, positions, total, false);
@@ -720,8 +737,9 @@ int append(ContextBase *ctx, const spd_shape *s, const spd_kv_view *v, const int
             return rc;
         a.items = reinterpret_cast<const AppendItem *>(e->dev);
     }
-    with_turn_kernel(s->dtype, s->head_dim, rope && rope->adjacent, [&](auto dt, auto d, auto adjacent) {
-        hipLaunchKernelGGL((append_kernel<dt(), d(), adjacent()>), dim3((unsigned)n_items), dim3(256), 0, stream, a, given);
+    const bool once = total * token_bytes >= kOnceBytes;
+    with_turn_kernel(s->dtype, s->head_dim, rope && rope->adjacent, once, [&](auto dt, auto d, auto adjacent, auto once) {
+        hipLaunchKernelGGL((append_kernel<dt(), d(), adjacent(), once()>), dim3((unsigned)n_items), dim3(256), 0, stream, a, given);
     });
     SPD_TRY(ctx, hipGetLastError());
     return SPD_OK;
@@ -773,10 +791,12 @@ int spd_rotate(spd_ctx *ctx, int32_t dtype, int32_t head_dim, const spd_rope *ro
     a.x_stride = x_token_stride * es;
     a.y_stride = y_token_stride * es;
     a.n_heads = n_heads;
-    a.per_group = tokens_per_group(n_tokens, c->n_cus);
+    const int64_t token_bytes = (int64_t)n_heads * head_dim * es;
+    a.per_group = tokens_per_group(n_tokens, token_bytes, c->n_cus);
     const unsigned blocks = (unsigned)(((int64_t)n_tokens + a.per_group - 1) / a.per_group);
-    with_turn_kernel(dtype, head_dim, rope->adjacent != 0, [&](auto dt, auto d, auto adjacent) {
-        hipLaunchKernelGGL((rotate_kernel<dt(), d(), adjacent()>), dim3(blocks), dim3(256), 0, static_cast<hipStream_t>(hip_stream), a);
+    const bool once = n_tokens * token_bytes >= kOnceBytes;
+    with_turn_kernel(dtype, head_dim, rope->adjacent != 0, once, [&](auto dt, auto d, auto adjacent, auto once) {
+        hipLaunchKernelGGL((rotate_kernel<dt(), d(), adjacent(), once()>), dim3(blocks), dim3(256), 0, static_cast<hipStream_t>(hip_stream), a);
     });
     SPD_TRY(c, hipGetLastError());
     return SPD_OK;
