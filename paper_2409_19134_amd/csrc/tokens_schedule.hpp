@@ -250,39 +250,62 @@ struct TokTile {
     int32_t user, kv_head, row0, n_rows, steps, first;  // first: index into the spans
 };
 
-// Cuts tiles into stretches of at most `chunk` steps: how many stretches in all.
-inline int64_t stretches(const std::vector<TokTile> &tiles, int64_t chunk)
-{
-    int64_t n = 0;
-    for (const TokTile &t : tiles)
-        n += std::max<int64_t>(1, (t.steps + chunk - 1) / chunk);
-    return n;
-}
+// Tiles cut into stretches of at most `chunk` steps: how many stretches in all, and how long the longest is.
+struct Cut {
+    int64_t n = 0, longest = 0;
+    Cut(const std::vector<TokTile> &tiles, int64_t chunk)
+    {
+        for (const TokTile &t : tiles) {
+            const int64_t k = std::max<int64_t>(1, (t.steps + chunk - 1) / chunk);
+            n += k;
+            longest = std::max(longest, (t.steps + k - 1) / k);
+        }
+    }
+};
 
-// The stretch length: the shortest with which all stretches run at once, but no shorter than `least` steps (each costs a partial and its join).
-// Work beyond one round goes by `most`, or whole where a tile is no more than its share of the work: splitting then only costs.  (Few rows: one token of
-// 24 users over 8192-32768 keys, 64 query heads in groups of eight, us: stretches of up to 128 steps, a round and a half, 344, up to 512, one round, 323;
-// many rows: a chunk of 8192 tokens over 16384, tiles of up to 256 steps cut at 64 970 + 100 for the join, whole 934.)
-inline int64_t stretch_steps(const std::vector<TokTile> &tiles, int64_t at_once, int64_t least, int64_t most)
+// The longest stretch to cut tiles into, by what the call then takes in steps of one workgroup (`at_once` of them run side by side): tiles left whole, as long
+// as the longest or as the average and the unevenness at the end; one round of stretches, as long as the longest of them; several rounds,
+// shorter and so more even.  A stretch costs `overhead` steps (its start, its partial and the join).  No stretch is shorter than `least`.
+// Few rows, us per call by the stretches' length: 64 users of 512-4096 keys, 8 KV heads of 64 (512 tiles, 48 steps for each of 768 workgroups): one round of up to
+// 75 steps 84.6, 24 steps 65.5, 16 steps 63.7; 24 users of 8192-32768 keys, 8 KV heads (165 steps): one round of up to 183 343, 64 steps 354, 24 steps 368;
+// 16 users of 512-4096 keys (12 steps): one round of up to 13 34.7, 24 steps 37.8, 10 steps 38.2.
+// Many rows: 4096 causal tokens, 16 query heads of one KV head of 128, bf16 (512 tiles of up to 64 steps, 32 each on average): whole 104, 16 steps 116; 2048
+// tokens, 32 heads in groups of four, fp32 (the same steps): whole 473, 16 steps 394.
+inline int64_t stretch_steps(const std::vector<TokTile> &tiles, int64_t at_once, int64_t least, double overhead)
 {
-    int64_t total = 0, longest = 0;
-    for (const TokTile &t : tiles) {
+    int64_t total = 0;
+    for (const TokTile &t : tiles)
         total += t.steps;
-        longest = std::max<int64_t>(longest, t.steps);
+    const double average = (double)total / (double)at_once, uneven = 0.35;
+    const int64_t longest = Cut(tiles, (int64_t)1 << 40).longest;
+    if (longest <= least)
+        return least;
+    int64_t best = longest;
+    double time = std::max((double)longest, average + uneven * (double)longest);
+    if ((int64_t)tiles.size() < at_once) {  // the shortest with which one round takes them all
+        int64_t lo = least, hi = longest;
+        while (lo < hi) {
+            const int64_t mid = (lo + hi) / 2;
+            if (Cut(tiles, mid).n <= at_once)
+                hi = mid;
+            else
+                lo = mid + 1;
+        }
+        const double t = (double)Cut(tiles, lo).longest + overhead;
+        if (t < time) {
+            best = lo;
+            time = t;
+        }
     }
-    if (longest <= total / at_once)
-        return std::max<int64_t>(1, longest);
-    int64_t lo = least, hi = std::max(most, total / at_once);
-    if (stretches(tiles, hi) >= at_once)
-        return hi;
-    while (lo < hi) {
-        const int64_t mid = (lo + hi) / 2;
-        if (stretches(tiles, mid) <= at_once)
-            hi = mid;
-        else
-            lo = mid + 1;
+    for (int rounds : {2, 3, 5}) {
+        const int64_t c = std::max<int64_t>({least, 12, (int64_t)(average / rounds)});
+        const double t = average * (1 + overhead / (double)c) + overhead + uneven * (double)c;
+        if (c < longest && (double)Cut(tiles, c).n >= 2.5 * (double)at_once && t < 0.97 * time) {
+            best = c;
+            time = t;
+        }
     }
-    return lo;
+    return best;
 }
 
 constexpr int kXcds = 8;
@@ -334,7 +357,9 @@ inline void build_tok_tables(const spd_shape *s, const spd_kv_view *v, const std
         const bool many = k == (int)TokKernel::kMany;
         const int step = many ? many_keys(s->dtype) : kFewKeys;
         const int64_t at_once = (int64_t)n_cus * resident((TokKernel)k);
-        const int64_t chunk = stretch_steps(tl, at_once, 4, many ? 64 : 512);
+        // (a step of many rows is short for its partial's 64 KB; fp32 steps take longer)
+        const double overhead = k == (int)TokKernel::kFew16 ? 2.5 : many && s->dtype != SPD_F32 ? 10.0 : 5.0;
+        const int64_t chunk = stretch_steps(tl, at_once, 4, overhead);
         // Few rows: the longest stretches first.  The many kernel's tiles of one head read the same keys: they go to one XCD (workgroup i
         // runs on XCD i % 8), whose L2 then holds them; heads in order of their work, each to the XCD with least so far.  Where that would
         // leave XCDs idle (their number divides that of the heads badly, and these are few) a head's tiles are dealt out to several.
