@@ -419,7 +419,7 @@ int spd_append_tokens(spd_ctx *ctx, const spd_shape *shape, const spd_kv_view *v
  * not finite in its channel (infinite or NaN), and no others.
  */
 typedef struct spd_score {
-    float cap;              /* 0 (none) or positive, finite                                                         */
+    float cap;              /* 0 (none) or positive, at most 1e30, scale / cap neither subnormal nor near overflow  */
     const float *slopes;    /* DEVICE [Hq] finite, or NULL                                                          */
     int32_t causal;         /* 0 or 1                                                                               */
     int32_t window;         /* 0: unlimited, else 1 .. 2^30                                                         */
@@ -435,6 +435,7 @@ typedef struct spd_score {
  * partials merge with spd_lse_merge):
  *   A[t][h] = sum_k exp(s_k - lse) v_k,   lse[t][h] = ln sum_k exp(s_k)   over the keys that the query sees.
  *   n_new      HOST [n_users], 0 .. 2^30 (at most lens[u] where q_pos is NULL); T * Hq at most 2^31 - 1
+ *   view       as in the partial calls; token_stride and, paged, block_stride at most 2^28 bytes
  *   q          DEVICE [T][Hq][d], the tokens q_token_stride elements apart (as in spd_append_tokens)
  *   out        DEVICE [T][Hq][d] of out_dtype: SPD_F32, or shape->dtype (each value rounded once; 16-bit probabilities
  *              then enter the second product rounded once too)

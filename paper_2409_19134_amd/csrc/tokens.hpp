@@ -229,33 +229,27 @@ struct RunMask {
     __device__ __forceinline__ bool sees(const RowMask &r, int i) const { return (unsigned)(m + i) < r.mn || (unsigned)(p + i) < r.pn; }
 };
 
-// tanh from its definition by one exponential, (1 - e) / (1 + e) with e = exp(-2|x|): off by a few 1e-8 of 1.  PRECISE: near zero, where that is
-// much of the value, the series instead (x^13's term is 2e-9 of x at 0.3).
-template <bool PRECISE>
+// tanh from its definition by one exponential, (1 - e) / (1 + e) with e = exp(-2|x|): off by a few 1e-8 of 1.  Near zero, where that is much of
+// the value (a cap far above the scores), the series instead (x^13's term is 2e-9 of x at 0.3).
 __device__ __forceinline__ float tanh_of(float x)
 {
-    const float a = fabsf(x);
+    const float a = fabsf(x), y = x * x;
     const float e = fast_exp2(-2.f * kLog2e * a);
-    float t = copysignf((1.f - e) * fast_rcp(1.f + e), x);
-    if constexpr (PRECISE) {
-        const float y = x * x;
-        float p = fmaf(y, -1382.f / 155925.f, 62.f / 2835.f);
-        p = fmaf(y, p, -17.f / 315.f);
-        p = fmaf(y, p, 2.f / 15.f);
-        p = fmaf(y, p, -1.f / 3.f);
-        t = a < 0.3f ? fmaf(x * y, p, x) : t;
-    }
-    return t;
+    float p = fmaf(y, -1382.f / 155925.f, 62.f / 2835.f);
+    p = fmaf(y, p, -17.f / 315.f);
+    p = fmaf(y, p, 2.f / 15.f);
+    p = fmaf(y, p, -1.f / 3.f);
+    return a < 0.3f ? fmaf(x * y, p, x) : copysignf((1.f - e) * fast_rcp(1.f + e), x);
 }
 
 // A product <q, k> with its cap and bias, in units of log2 (MOD) or as it is (the factor c comes with the exponential then).  apart: the query's position
 // less the key's.
-template <bool MOD, bool PRECISE>
+template <bool MOD>
 __device__ __forceinline__ float modified(float s, const ScoreArgs &a, const RowMask &r, int apart)
 {
     if constexpr (!MOD)
         return s;
-    float x = a.cap_out != 0.f ? tanh_of<PRECISE>(s * a.cap_in) * a.cap_out : s * a.c;
+    float x = a.cap_out != 0.f ? tanh_of(s * a.cap_in) * a.cap_out : s * a.c;
     if (a.slopes)
         x = fmaf(-r.slope2, (float)(abs(apart) - r.dist0), x);
     return x;

@@ -226,7 +226,7 @@ __global__ __launch_bounds__(256, 2) void tokens_few_kernel(const TokArgs a)
             const RunMask run(mask[nt], t0);
 #pragma unroll
             for (int e = 0; e < NE; ++e)
-                x[e] = modified<MOD, true>(s[e / 4][e % 4], a.score, mask[nt], run.q - e);
+                x[e] = modified<MOD>(s[e / 4][e % 4], a.score, mask[nt], run.q - e);
             if (masked)
 #pragma unroll
                 for (int e = 0; e < NE; ++e)

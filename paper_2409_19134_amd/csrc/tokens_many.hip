@@ -57,9 +57,11 @@ __device__ __forceinline__ uint32_t lds_address(const char *p) { return (uint32_
 __device__ __forceinline__ void all_loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // What happens to a score.  kCapped: a cap alone, for results of 16 bits: two multiplications, an addition, an exponential and a reciprocal, of which
-// the softmax's own multiplication takes the last (the general form, with a copied sign and the bias, takes eleven; prompts of 900-4096 tokens
-// with 32 heads of 128, us per call, general / this: see below).  It is off by 2^-23 of the cap, which 24-bit results would show.
+// the softmax's own multiplication takes the last (the general form, with a copied sign, the series near zero and the bias, takes eighteen; four prompts of
+// 900-4096 tokens with 32 heads of 128, us per call: 335 / GENERAL).  It is off by 2^-23 of twice the cap: up to a cap of 64, 2^-16, little beside a rounded P's 2^-12
+// to 2^-9, but 24-bit results would show it, and a cap far above the scores would leave nothing of them.
 enum { kPlain = 0, kCapped = 1, kGeneral = 2 };
+constexpr float kCappedMost = 64.f * kLog2e;
 
 constexpr float kRaise = 8.f;   // log2 of what a row's largest P may be
 // P carries 2^kShift: fp16's keep to [2^-24, 65504] with a maximum of 2^(kRaise + 7)
@@ -281,7 +283,7 @@ __global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
                     if constexpr (MOD == kCapped)  // -1 / (1 + exp(2 s / cap)): twice the cap times that, and the cap, is cap tanh(s / cap)
                         x[nb][i] = fast_rcp(-1.f - fast_exp2(x[nb][i] * steep));
                     else
-                        x[nb][i] = modified<true, EXACT>(x[nb][i], a.score, mask, run.q - (nb * 32 + 8 * (i / 4) + i % 4));
+                        x[nb][i] = modified<true>(x[nb][i], a.score, mask, run.q - (nb * 32 + 8 * (i / 4) + i % 4));
                 }
         if (masked)
 #pragma unroll
@@ -426,7 +428,7 @@ void launch(bool modified, int64_t n_items, const TokArgs &a, hipStream_t stream
     const dim3 grid((unsigned)n_items), block(256);
     if (!modified)
         hipLaunchKernelGGL((tokens_many_kernel<DT, D, EXACT, kPlain>), grid, block, 0, stream, a);
-    else if (!EXACT && !a.score.slopes)
+    else if (!EXACT && !a.score.slopes && a.score.cap_out <= kCappedMost)
         hipLaunchKernelGGL((tokens_many_kernel<DT, D, EXACT, EXACT ? kGeneral : kCapped>), grid, block, 0, stream, a);
     else
         hipLaunchKernelGGL((tokens_many_kernel<DT, D, EXACT, kGeneral>), grid, block, 0, stream, a);

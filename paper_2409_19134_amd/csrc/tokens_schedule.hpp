@@ -103,6 +103,8 @@ inline int validate_append(const spd_shape *s, const spd_kv_view *v, const int32
     return SPD_OK;
 }
 
+constexpr float kMaxCap = 1e30f;  // cap log2(e) stays finite, and what scale / cap times a product loses below 2^-126 is below 2^-26 of a score
+
 inline int32_t first_key_position(const spd_score *c, int u) { return c && c->k_pos ? c->k_pos[u] : 0; }
 
 inline int validate_tokens(const spd_shape *s, const void *q, int64_t q_stride, const spd_kv_view *v, const int32_t *n_new, const spd_score *c,
@@ -118,10 +120,13 @@ inline int validate_tokens(const spd_shape *s, const void *q, int64_t q_stride, 
     // the kernels' products of a token's or page's number and its stride are 32 by 32 bits
     if (v->token_stride > kMaxStrideBytes / elt_size(s->dtype) || (v->block_size != 0 && v->block_stride > kMaxStrideBytes / elt_size(s->dtype)))
         return SPD_ERR_ALIGN;
-    if (c && (!(c->cap >= 0.f) || !std::isfinite(c->cap) || (c->causal != 0 && c->causal != 1)))
+    if (c && (!(c->cap >= 0.f) || !(c->cap <= kMaxCap) || (c->causal != 0 && c->causal != 1)))
         return SPD_ERR_SHAPE;
-    if (c && c->cap > 0.f && !std::isfinite(std::fabs(s->scale) / c->cap))  // (a subnormal cap)
-        return SPD_ERR_SHAPE;
+    if (c && c->cap > 0.f && s->scale != 0.f) {  // the kernels' factor scale / cap in all its 24 bits, four times it finite
+        const float in = std::fabs(s->scale) / c->cap;
+        if (!std::isnormal(in) || !std::isfinite(4.f * in))
+            return SPD_ERR_SHAPE;
+    }
     if (c && (c->window < 0 || c->window > kMaxPosition))
         return SPD_ERR_LEN;
     int64_t total = 0;

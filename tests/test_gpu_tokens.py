@@ -445,3 +445,23 @@ def test_refusals_reach_no_kernel(ctx):
         assert e.value.code == code
     torch.cuda.synchronize()
     assert bool((out == 5.0).all()) and bool((lse == 5.0).all())
+
+
+@pytest.mark.parametrize("dtype,out", [("f32", "f32"), ("bf16", "f32"), ("bf16", "same"), ("f16", "same")])
+@pytest.mark.parametrize("cap", [1e4, 1e6, 1e30])
+@pytest.mark.parametrize("new", [[2, 1], [9], [300]])
+@pytest.mark.parametrize("slopes", [False, True])
+def test_a_cap_far_above_the_scores_changes_nothing(ctx, dtype, out, cap, new, slopes):
+    """cap tanh(s / cap) = s (1 - (s / cap)^2 / 3 + ..): of scores below 64, a 24-bit rounding at most, so held to the bounds without a cap."""
+    p = Problem((32, 8, 128), dtype, "hnd", new, [700], dict(slopes=slopes), out, seed=23).store()
+    want = p.exact()
+    assert 64.0 > p.most      # (a sum of magnitudes: the scores are smaller)
+    p.score = p.spd.Score(cap=cap, slopes=None if p.slopes is None else p.slopes.float().to(DEV), causal=True, k_pos=p.k_pos)
+    p.exact = lambda: want
+    p.check(*p.call(ctx))
+
+
+def test_caps_around_the_short_form(ctx):
+    for cap in (0.01, 1.0, 63.0, 64.0, 65.0, 200.0):
+        p = Problem((32, 8, 128), "bf16", "hnd", [200], [500], dict(cap=cap), "same", seed=24).store()
+        p.check(*p.call(ctx))

@@ -162,3 +162,15 @@ def test_calls_need_a_context():
     assert b.lib.spd_rotate(None, 1, 64, C.byref(r), 1, P, 8, P, 512, P, 512, 0, None) == spd.SPD_ERR_NULL
     assert b.lib.spd_append_tokens(None, C.byref(s), C.byref(v.struct), n[1], None, None, None, 0, None, P, 128, P, 128, None) == spd.SPD_ERR_NULL
     assert b.lib.spd_partial_attn_tokens(None, C.byref(s), P, 512, C.byref(v.struct), n[1], None, P, 0, P, None) == spd.SPD_ERR_NULL
+
+
+def test_refusals_of_caps_and_strides():
+    """Caps whose factors would not be finite or lose bits; strides whose products with a token's number the kernels cannot hold."""
+    S, A = spd.SPD_ERR_SHAPE, spd.SPD_ERR_ALIGN
+    for cap in (1.001e30, 3e38, 1e-39):      # (0.125 / 1e-39 four times is past the largest value)
+        assert _tokens(score=spd.Score(cap=cap)) == S, cap
+    assert _tokens(score=spd.Score(cap=1e30)) == 0 and _tokens(score=spd.Score(cap=1e-30)) == 0
+    assert _tokens(shape=_shape(scale=1e-9), score=spd.Score(cap=1e30)) == S         # scale / cap below 2^-126
+    assert _tokens(shape=_shape(scale=0.0), score=spd.Score(cap=1e30)) == 0
+    most = (1 << 28) // 2                                                            # in 16-bit elements
+    assert _tokens(view=View(token_stride=most, head_stride=64)) == 0 and _tokens(view=View(token_stride=most + 8, head_stride=64)) == A
