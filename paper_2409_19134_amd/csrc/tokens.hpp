@@ -242,17 +242,19 @@ __device__ __forceinline__ float tanh_of(float x)
     return a < 0.3f ? fmaf(x * y, p, x) : copysignf((1.f - e) * fast_rcp(1.f + e), x);
 }
 
-// A product <q, k> with its cap and bias, in units of log2 (MOD) or as it is (the factor c comes with the exponential then).  apart: the query's position
-// less the key's.
+// A product <q, k> with its cap, in units of log2.
+__device__ __forceinline__ float capped(float s, const ScoreArgs &a) { return tanh_of(s * a.cap_in) * a.cap_out; }
+// ... and the bias of a key `apart` positions from its query, less that of the row's nearest key.
+__device__ __forceinline__ float biased(float x, const RowMask &r, int apart) { return fmaf(-r.slope2, (float)(abs(apart) - r.dist0), x); }
+
+// A product <q, k> with its cap and bias, in units of log2 (MOD) or as it is (the factor c comes with the exponential then).
 template <bool MOD>
 __device__ __forceinline__ float modified(float s, const ScoreArgs &a, const RowMask &r, int apart)
 {
     if constexpr (!MOD)
         return s;
-    float x = a.cap_out != 0.f ? tanh_of(s * a.cap_in) * a.cap_out : s * a.c;
-    if (a.slopes)
-        x = fmaf(-r.slope2, (float)(abs(apart) - r.dist0), x);
-    return x;
+    const float x = a.cap_out != 0.f ? capped(s, a) : s * a.c;
+    return a.slopes ? biased(x, r, apart) : x;
 }
 
 // A key that a row does not see must not reach it, and zero times infinity is NaN: where some row does not see some key, non-finite values

@@ -275,16 +275,37 @@ __global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
     auto masks = [&](f32x16 (&x)[NB], int kt, float top) __attribute__((always_inline)) {
         const RunMask run(mask, kt + 4 * h);
         const bool masked = kt < mine.full_lo || kt + BN > mine.full_hi;
-        if constexpr (MOD != kPlain)
+        if constexpr (MOD == kCapped) {  // -1 / (1 + exp(2 s / cap)): twice the cap times that, and the cap, is cap tanh(s / cap)
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    if constexpr (MOD == kCapped)  // -1 / (1 + exp(2 s / cap)): twice the cap times that, and the cap, is cap tanh(s / cap)
-                        x[nb][i] = fast_rcp(-1.f - fast_exp2(x[nb][i] * steep));
-                    else
-                        x[nb][i] = modified<true>(x[nb][i], a.score, mask, run.q - (nb * 32 + 8 * (i / 4) + i % 4));
-                }
+                for (int i = 0; i < 16; ++i)
+                    x[nb][i] = fast_rcp(-1.f - fast_exp2(x[nb][i] * steep));
+        } else if constexpr (MOD == kGeneral) {
+            // Before all of the wave's queries a key's distance grows by one from key to key: the bias is a line, one fma per score.
+            const bool before = a.score.slopes && __builtin_amdgcn_ballot_w64(run.q < BN - 1) == 0;
+            const float nearest = mask.slope2 * (float)(mask.dist0 - run.q);
+            const float f = a.score.cap_out != 0.f ? 1.f : a.score.c;
+            if (a.score.cap_out != 0.f)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        x[nb][i] = capped(x[nb][i], a.score);
+            if (before) {
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        x[nb][i] = fmaf(x[nb][i], f, fmaf(mask.slope2, (float)(nb * 32 + 8 * (i / 4) + i % 4), nearest));
+            } else if (a.score.slopes) {
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        x[nb][i] = biased(x[nb][i] * f, mask, run.q - (nb * 32 + 8 * (i / 4) + i % 4));
+            }
+        }
         if (masked)
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
