@@ -7,6 +7,10 @@
 // as three bf16 or two fp16 terms (24 and 22 bits), since partials are fp32 and V is read once however many products it goes through.
 // Rows differ in what they see (causal order among the new tokens, windows, documents): a step that not every row sees whole is masked
 // element by element, steps that none sees are left out.
+// Measured (a read of 8 GB: 6.8 TB/s): one token of 24 users over 8192-32768 keys, 64 query heads in groups of eight, fp16 with a cap, 2.07 GB: 323 us, 6.4 TB/s;
+// six tokens of 24 users over 900-8000 keys, groups of four, pages of 64, bf16, 459 MB: 85 us, 5.4 TB/s, of which the join is 5; one token of 16 users
+// over 512-4096 keys with a distance bias, pages of 16, 150 MB: 33 us, 4.5 TB/s, the join 4.5: stretches of at most 13 steps, so a start (a table's
+// entry, the page numbers, then the first keys: 3 us one behind the other) for a few us of loads.  One user's token over 1531 keys: 11 us, launches.
 #include "partial_mfma.hpp"
 #include "tokens.hpp"
 
