@@ -286,11 +286,11 @@ def _token_rows(t: torch.Tensor, n_tokens: int, n_heads: int, head_dim: int) -> 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _stream_ptr(stream) -> Optional[int]:
-    if stream is None:
+def _stream_ptr(stream, device: Optional[int] = None) -> Optional[int]:
+    if stream is None:      # torch's current one, of the device given or the current one
         if _raw_stream is not None:
-            return _raw_stream(torch.cuda.current_device()) or None
-        stream = torch.cuda.current_stream()
+            return _raw_stream(torch.cuda.current_device() if device is None else device) or None
+        stream = torch.cuda.current_stream(device)
     return C.c_void_p(stream.cuda_stream)
 
 
@@ -315,6 +315,11 @@ class Context:
             self.close()
         except Exception:
             pass
+
+    def _here(self, *tensors):
+        """The tensors lie on the context's device (a kernel must not follow other addresses)."""
+        for t in tensors:
+            assert t is None or t.get_device() == self.device
 
     def _check(self, rc: int, where: str):
         if rc != SPD_OK:
@@ -508,10 +513,11 @@ class Context:
         T, H, d = x.shape
         if y is None:
             y = torch.empty((T, H, d), device=x.device, dtype=x.dtype)
-        assert y.dtype == x.dtype and y.device == x.device
+        assert y.dtype == x.dtype
+        self._here(x, y, positions, rope.inv_freq)
         assert positions.dtype is torch.int32 and positions.is_contiguous() and positions.numel() == rope.struct.n_axes * T
         rc = lib.spd_rotate(self.handle, _DTYPE_CODES[x.dtype], d, C.byref(rope.struct), T, positions.data_ptr(), H, x.data_ptr(),
-                            _token_rows(x, T, H, d), y.data_ptr(), _token_rows(y, T, H, d), int(bool(transposed)), _stream_ptr(stream))
+                            _token_rows(x, T, H, d), y.data_ptr(), _token_rows(y, T, H, d), int(bool(transposed)), _stream_ptr(stream, self.device))
         self._check(rc, "spd_rotate")
         return y
 
@@ -523,6 +529,9 @@ class Context:
         Hq, H, d, dtype = shape.n_q_heads, shape.n_kv_heads, shape.head_dim, _CODE_DTYPES[shape.dtype]
         ks, vs, qs = _token_rows(k_new, T, H, d), _token_rows(v_new, T, H, d), 0
         assert k_new.dtype == v_new.dtype == dtype
+        self._here(k_new, v_new, q, q_out if q is not None else None)
+        if rope is not None:
+            self._here(positions, rope.inv_freq)
         assert rope is None or (positions.dtype is torch.int32 and positions.is_contiguous() and positions.numel() == rope.struct.n_axes * T)
         if q is not None:
             qs = _token_rows(q, T, Hq, d)
@@ -532,7 +541,7 @@ class Context:
         rc = lib.spd_append_tokens(self.handle, C.byref(shape), C.byref(view.struct), counts.ctypes.data,
                                    None if rope is None else C.byref(rope.struct), None if rope is None else positions.data_ptr(),
                                    None if q is None else q.data_ptr(), qs, None if q is None else q_out.data_ptr(), k_new.data_ptr(), ks,
-                                   v_new.data_ptr(), vs, _stream_ptr(stream))
+                                   v_new.data_ptr(), vs, _stream_ptr(stream, self.device))
         self._check(rc, "spd_append_tokens")
         return q_out if q is not None else None
 
@@ -549,11 +558,13 @@ class Context:
         qs = _token_rows(q, T, Hq, d)
         assert q.dtype == dtype and out.is_contiguous() and out.shape == (T, Hq, d) and out.dtype in (torch.float32, dtype)
         assert lse.is_contiguous() and lse.shape == (T, Hq) and lse.dtype is torch.float32
+        self._here(q, out, lse)
         if score is not None:
             score.check(view.struct.n_users, T, Hq)
+            self._here(score.slopes, score.ranges)
         rc = lib.spd_partial_attn_tokens(self.handle, C.byref(shape), q.data_ptr(), qs, C.byref(view.struct), counts.ctypes.data,
                                          None if score is None else C.byref(score.struct), out.data_ptr(), _DTYPE_CODES[out.dtype],
-                                         lse.data_ptr(), _stream_ptr(stream))
+                                         lse.data_ptr(), _stream_ptr(stream, self.device))
         self._check(rc, "spd_partial_attn_tokens")
         return out, lse
 

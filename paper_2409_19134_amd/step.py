@@ -140,7 +140,8 @@ class TokenStep:
 
     `view` is the cache that takes the tokens: its lengths already count them, n_new[u] of user u.  With `prompt` (the other owner's view of
     the same users) the sequence begins there: the tokens attend to both caches, and the two partials are merged as in Theorem 1.  `rope`, and the
-    keywords of Score that concern a sequence (cap, slopes, causal, window, prefix, ranges), are the model's.  Holds the result buffers."""
+    keywords of Score that concern a sequence (cap, slopes, causal, window, prefix, ranges), are the model's.  Holds the result buffers.  The views'
+    lengths are read at every run, so a loop may move them on."""
 
     def __init__(self, ctx: Context, dtype, n_q_heads: int, n_kv_heads: int, head_dim: int, scale: float, view: KVView, n_new,
                  rope: Rope = None, prompt: KVView = None, device="cuda:0", **score):
@@ -152,12 +153,12 @@ class TokenStep:
         self.q = torch.empty((T, n_q_heads, head_dim), device=device, dtype=dtype)
         self.a_out, self.lse_out = torch.empty((T, n_q_heads, head_dim), **f32), torch.empty((T, n_q_heads), **f32)
         begin = None if prompt is None else prompt.lens
-        self.score_out = Score(k_pos=begin, **score)
+        self.score_out = Score(k_pos=begin, **score)      # (the same array: what the caller makes of the lengths holds from the next run on)
         if prompt is not None:
             assert prompt.struct.n_users == view.struct.n_users
             self.a_in, self.y = (torch.empty((T, n_q_heads, head_dim), **f32) for _ in range(2))
             self.lse_in, self.lse, self.w_in = (torch.empty((T, n_q_heads), **f32) for _ in range(3))
-            self.score_in = Score(q_pos=begin + view.lens - self.n_new, **score)
+            self.score_in = Score(q_pos=np.zeros_like(begin), **score)
 
     def run(self, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, positions: torch.Tensor = None, stream=None):
         """Enqueues the step; returns (attention, its log-sum-exp).  q, k_new, v_new: [T][heads][d] as the projection leaves them; positions
@@ -169,6 +170,7 @@ class TokenStep:
         c.spd_partial_attn_tokens(self.shape, q, self.view, self.n_new, self.score_out, self.a_out, self.lse_out, stream=stream)
         if self.prompt is None:
             return self.a_out, self.lse_out
+        np.add(self.prompt.lens, self.view.lens - self.n_new, out=self.score_in.per_user["q_pos"])
         c.spd_partial_attn_tokens(self.shape, q, self.prompt, self.n_new, self.score_in, self.a_in, self.lse_in, stream=stream)
         c.spd_lse_merge(self.a_in, self.lse_in, self.a_out, self.lse_out, self.y, self.lse, self.w_in, stream)
         return self.y, self.lse

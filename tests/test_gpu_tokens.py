@@ -465,3 +465,53 @@ def test_caps_around_the_short_form(ctx):
     for cap in (0.01, 1.0, 63.0, 64.0, 65.0, 200.0):
         p = Problem((32, 8, 128), "bf16", "hnd", [200], [500], dict(cap=cap), "same", seed=24).store()
         p.check(*p.call(ctx))
+
+
+def test_a_token_step_follows_its_view(ctx):
+    """One TokenStep run again and again while the view's lengths (a host array that the caller owns) move on: the queries' positions over the prompt move with
+    them, which a window shows."""
+    import paper_2409_19134_amd as spd
+    Hq, H, d, dt, prompt, steps, window = 8, 2, 64, torch.float32, [70, 1, 133], 6, 40
+    gen = torch.Generator().manual_seed(29)
+    q, k, v = ([torch.randn((p + steps, h, d), generator=gen) for p in prompt] for h in (Hq, H, H))
+    private = ref.Cache(spd, [x[:p] for x, p in zip(k, prompt)], [x[:p] for x, p in zip(v, prompt)], "nhd", DEV)
+    room = [torch.zeros((steps, H, d)) for _ in prompt]
+    public = ref.Cache(spd, room, room, "nhd", DEV)
+    view = spd.KVView([0] * 3, H * d, d, k=list(public.k), v=list(public.v))
+    step = spd.TokenStep(ctx, dt, Hq, H, d, 0.125, view, [1] * 3, prompt=private.view, window=window)
+    for i in range(steps):
+        view.lens += 1
+        rows = [torch.stack([t[u][p + i] for u, p in enumerate(prompt)]).to(DEV) for t in (q, k, v)]
+        got, lse = step.run(*rows)
+        torch.cuda.synchronize()
+        for u, p in enumerate(prompt):
+            end = p + i + 1
+            a, want, b, most = ref.attend(q[u][end - 1:end], k[u][:end], v[u][:end], ref.visible(1, end, end - 1, 0, True, window), 0.125)
+            # (d + 4) roundings of a score, twice for the two partials' weights, and the 24-bit sums
+            delta = 2 ** -24 * (2 * (d + 4) * most + 256)
+            assert bool(((got[u:u + 1].double().cpu() - a).abs() <= (2 * delta + end * 2 ** -24) * b + 1e-6).all()), i
+            assert bool(((lse[u:u + 1].double().cpu() - want).abs() <= delta + end * 2 ** -24 + 8 * 2 ** -24 * want.abs()).all()), i
+
+
+def test_tensors_elsewhere_are_refused(ctx):
+    """Host tensors, whose addresses a kernel must not follow, do not get that far."""
+    import paper_2409_19134_amd as spd
+    p = Problem((8, 2, 64), "bf16", "hnd", [1, 2], [30, 40], dict(), "f32", seed=2).store()
+    q = p.q.to(DEV)
+    for args in ((p.q, spd.Score()), (q, spd.Score(slopes=torch.ones(8))), (q, spd.Score(ranges=torch.zeros((3, 2), dtype=torch.int32)))):
+        with pytest.raises(AssertionError):
+            ctx.spd_partial_attn_tokens(p.shape, args[0], p.cache.view, p.new, args[1])
+    for out, lse in ((torch.empty((3, 8, 64)), None), (None, torch.empty((3, 8)))):
+        with pytest.raises(AssertionError):
+            ctx.spd_partial_attn_tokens(p.shape, q, p.cache.view, p.new, None, out, lse)
+    inv, places = torch.ones(32), torch.zeros((1, 3), dtype=torch.int32)
+    k = p.cache.view
+    new = torch.zeros((3, 2, 64), dtype=torch.bfloat16)
+    for rope, pos, x in ((spd.Rope(inv), places.to(DEV), q), (spd.Rope(inv.to(DEV)), places, q), (spd.Rope(inv.to(DEV)), places.to(DEV), p.q)):
+        with pytest.raises(AssertionError):
+            ctx.spd_rotate(rope, x, pos)
+        with pytest.raises(AssertionError):
+            ctx.spd_append_tokens(p.shape, k, p.new, new.to(DEV), new.to(DEV), rope, pos, x)
+    for a, b in ((new, new.to(DEV)), (new.to(DEV), new)):
+        with pytest.raises(AssertionError):
+            ctx.spd_append_tokens(p.shape, k, p.new, a, b)
