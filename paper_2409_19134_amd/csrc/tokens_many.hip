@@ -15,11 +15,12 @@
 // barrier a tile.  16-byte pieces of a row are stored at places xor-ed with the row's number, so that neither
 // the reads of K (16 bytes of eight rows at once) nor the transposed reads of V (32 bytes of four rows) meet in a bank.
 // Masks: a tile that all rows of a wave see whole costs nothing, others are masked element by element, tiles that no row sees are left out.
-// Measured, 32 query heads in groups of four of 128 channels, bf16, results in bf16: 8192 tokens of documents over a cache of 16384 941 us, 1.03 PFLOP/s of
-// what the masks leave; 16384 causal tokens 2014 us, 1.09; 4096 causal tokens 166 us, 0.83 (half the tiles wait for the longest).  A library product of 8192^3
+// Measured, 32 query heads in groups of four of 128 channels, bf16, results in bf16: 8192 tokens of documents over a cache of 16384 932-970 us, 1.0 PFLOP/s
+// of what the masks leave; 16384 causal tokens 1956-2060 us, 1.07-1.12; 4096 causal tokens 161-170 us, 0.83: two tiles to a place, of which the last to end
+// leave their neighbours' places empty for 30 us, and 3 us to begin a tile, 3 to end it.  A library product of 8192^3
 // reaches 1.12.  Of the first (966 when it was taken apart) the loads are 118, the exponentials and maxima 104, LDS reads 24; matrix instructions and
 // barriers alone need 673.  Tried: the next tile's scores between this tile's weights, 962-988; one V buffer and three waves per SIMD, spills, 1134.
-// fp32: 2048 causal tokens 393 us, 87 TFLOP/s (a library product: 154; the matrix units are busy 71 % of a busy unit's time, and tiles of 128 rows
+// fp32: 2048 causal tokens 365 us, 94 TFLOP/s (a library product: 154; the matrix units are busy 71 % of a busy unit's time, and tiles of 128 rows
 // compute what the diagonal then masks).
 #include "tokens.hpp"
 
@@ -64,7 +65,7 @@ __device__ __forceinline__ void all_loads_done() { asm volatile("s_waitcnt vmcnt
 
 // What happens to a score.  kCapped: a cap alone, for results of 16 bits: two multiplications, an addition, an exponential and a reciprocal, of which
 // the softmax's own multiplication takes the last (the general form, with a copied sign, the series near zero and the bias, takes eighteen; four prompts of
-// 900-4096 tokens with 32 heads of 128, us per call: 335, generally 421).  It is off by 2^-23 of twice the cap: up to a cap of 64, 2^-16, little beside a rounded P's 2^-12
+// 900-4096 tokens with 32 heads of 128, us per call: 330, generally 421).  It is off by 2^-23 of twice the cap: up to a cap of 64, 2^-16, little beside a rounded P's 2^-12
 // to 2^-9, but 24-bit results would show it, and a cap far above the scores would leave nothing of them.
 enum { kPlain = 0, kCapped = 1, kGeneral = 2 };
 constexpr float kCappedMost = 64.f * kLog2e;

@@ -365,11 +365,16 @@ inline void build_tok_tables(const spd_shape *s, const spd_kv_view *v, const std
         // (a step of many rows is short for its partial's 64 KB; fp32 steps take longer)
         const double overhead = k == (int)TokKernel::kFew16 ? 2.5 : many && s->dtype != SPD_F32 ? 10.0 : 5.0;
         const int64_t chunk = stretch_steps(tl, at_once, 4, overhead);
-        // Few rows: the longest stretches first.  The many kernel's tiles of one head read the same keys: they go to one XCD (workgroup i
+        // The longest stretches first.  The many kernel's tiles of one head read the same keys: they go to one XCD (workgroup i
         // runs on XCD i % 8), whose L2 then holds them; heads in order of their work, each to the XCD with least so far.  Where that would
         // leave XCDs idle (their number divides that of the heads badly, and these are few) a head's tiles are dealt out to several.
-        // Within a head the last rows, whose causal part is longest, come first.
-        std::vector<std::vector<TokItem>> queue(many ? kXcds : 1);
+        // (Head after head on an XCD, so that fewer share its L2 at a time, us against this: 4096 causal tokens, 24 heads of 64 with their own KV heads
+        // 116 / 84; four prompts of 900-4096 tokens 340 / 331; 16384 tokens, 32 heads of 128 with their own KV heads, 8 MB each, 2106 / 2090.)
+        struct Queued {
+            TokItem item;
+            int32_t steps;
+        };
+        std::vector<std::vector<Queued>> queue(many ? kXcds : 1);
         std::vector<int64_t> load(queue.size(), 0);
         std::vector<int64_t> weight(plan.size() * (size_t)Hkv, 0);  // of a user's head
         for (const TokTile &t : tl)
@@ -414,25 +419,23 @@ inline void build_tok_tables(const spd_shape *s, const spd_kv_view *v, const std
                 }
                 it.to_len = s1 > s0 && j == n - 1 && it.k_end == plan[(size_t)t.user].len;
                 it.slot = n > 1 ? (int32_t)(slot + j) : -1;
-                queue[q].push_back(it);
+                queue[q].push_back(Queued{it, s1 - s0});
             }
             if (n > 1) {
                 T.joins[k].push_back(TokJoin{t.user, t.kv_head, t.row0, t.n_rows, (int32_t)slot, (int32_t)n, {0, 0}});
                 T.slots[k] += n;
             }
         }
-        if (!many) {
-            T.items[k] = std::move(queue[0]);
-            continue;
-        }
         size_t longest = 0;
-        for (const auto &x : queue)
+        for (auto &x : queue) {
+            std::stable_sort(x.begin(), x.end(), [](const Queued &a, const Queued &b) { return a.steps > b.steps; });
             longest = std::max(longest, x.size());
+        }
         const TokItem nothing = {0, 0, 0, 0, 0, 0, -1, 0};
-        T.items[k].reserve(longest * kXcds);
+        T.items[k].reserve(longest * queue.size());
         for (size_t i = 0; i < longest; ++i)
             for (const auto &x : queue)
-                T.items[k].push_back(i < x.size() ? x[i] : nothing);
+                T.items[k].push_back(i < x.size() ? x[i].item : nothing);
     }
 }
 
