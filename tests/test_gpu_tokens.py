@@ -515,3 +515,28 @@ def test_tensors_elsewhere_are_refused(ctx):
     for a, b in ((new, new.to(DEV)), (new.to(DEV), new)):
         with pytest.raises(AssertionError):
             ctx.spd_append_tokens(p.shape, k, p.new, a, b)
+
+
+@pytest.mark.parametrize("dtype,out", [("bf16", "f32"), ("f16", "same"), ("f32", "f32")])
+@pytest.mark.parametrize("new", [[2, 1, 3, 1], [9, 20, 7, 12], [70, 200, 33, 129]])
+@pytest.mark.parametrize("score", [dict(causal=True), dict(causal=False, slopes=True), dict(causal=False, window=60, slopes=True, cap=8.0),
+                                   dict(causal=True, window=60, prefix=True, slopes=True)], ids=["causal", "slopes", "window", "prefix"])
+def test_queries_before_among_and_after_the_keys(ctx, dtype, out, new, score):
+    """Positions of the queries wherever the caller says: before every key of the view, among them, right behind them and far behind."""
+    p = Problem((8, 2, 128), dtype, "nhd", new, [300, 150, 1, 420], score, out, elsewhere=True, seed=31)
+    p.k_pos = [500, 90, 40, 0]
+    p.q_pos = [3, 120, 41, 900]
+    if p.prefix is not None:
+        p.prefix = [600, 0, 41, 7]
+    p.store()
+    p.check(*p.call(ctx))
+
+
+def test_a_thousand_users(ctx):
+    """More users than a table's usual room, most with one token, some with none."""
+    new = [u % 3 for u in range(1100)]
+    p = Problem((4, 4, 64), "bf16", "hnd", new, [u % 7 for u in range(1100)], dict(cap=9.0), "f32", seed=33).store()
+    got = p.call(ctx)
+    p.check(*got)
+    again = p.call(ctx)
+    assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
