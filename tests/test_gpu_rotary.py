@@ -208,3 +208,22 @@ def test_append_recorded_in_a_graph(ctx):
             for u in range(users):
                 at = 19 + u % 20
                 assert torch.equal(got[0][u, :, at], k[u, :, at]) and torch.equal(got[1][u, :, at], v[u, :, at])
+
+
+def test_rotate_recorded_without_a_run_before(ctx):
+    """A rotation needs nothing of the context: it can be recorded at once, and replays follow their inputs."""
+    import paper_2409_19134_amd as spd
+    x, y = torch.randn((37, 6, 128), device=DEV).bfloat16(), torch.zeros((37, 6, 128), device=DEV, dtype=torch.bfloat16)
+    pos = torch.zeros((2, 37), dtype=torch.int32, device=DEV)
+    rope = spd.Rope(torch.linspace(1.0, 0.001, 64, device=DEV), 2, [j % 2 for j in range(64)])
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        ctx.spd_rotate(rope, x, pos, y)
+    for i in range(4):
+        x.normal_()
+        pos.random_(0, 1 << 20)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, ctx.spd_rotate(rope, x, pos))

@@ -540,3 +540,38 @@ def test_a_thousand_users(ctx):
     p.check(*got)
     again = p.call(ctx)
     assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
+
+
+def test_a_token_step_recorded_whole(ctx):
+    """Append, attention over both owners' caches and the merge in one graph: replays follow the tokens, their positions and the caches, with eager calls of
+    the same context in between."""
+    import paper_2409_19134_amd as spd
+    Hq, H, d, dt, prompt, new = 8, 2, 128, torch.bfloat16, [400, 3, 90], [4, 1, 30]
+    gen = torch.Generator().manual_seed(37)
+    rand = lambda l: torch.randn((l, H, d), generator=gen).to(dt)  # noqa: E731
+    private = ref.Cache(spd, [rand(l) for l in prompt], [rand(l) for l in prompt], "paged_nhd16", DEV)
+    public = ref.Cache(spd, [rand(l + 9) for l in new], [rand(l + 9) for l in new], "hnd", DEV)
+    rope = spd.Rope(torch.linspace(1.0, 0.001, 64, device=DEV))
+    T = sum(new)
+    q, k, v = (torch.randn((T, h, d), device=DEV).to(dt) for h in (Hq, H, H))
+    pos = torch.arange(T, dtype=torch.int32, device=DEV)
+    step = spd.TokenStep(ctx, dt, Hq, H, d, 0.088, public.view, new, rope, private.view, cap=30.0, window=200)
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        step.run(q, k, v, pos)
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=stream):
+            y, lse = step.run(q, k, v, pos)
+    for i in range(4):
+        for t in (q, k, v):
+            t.normal_()
+        pos.add_(3)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = y.clone(), lse.clone()
+        y.zero_()
+        step.run(q, k, v, pos)
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], y) and torch.equal(got[1], lse) and bool(torch.isfinite(lse).all())
