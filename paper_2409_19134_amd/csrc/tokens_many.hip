@@ -20,8 +20,8 @@
 // leave their neighbours' places empty for 30 us, and 3 us to begin a tile, 3 to end it.  A library product of 8192^3
 // reaches 1.12.  Of the first (966 when it was taken apart) the loads are 118, the exponentials and maxima 104, LDS reads 24; matrix instructions and
 // barriers alone need 673.  Tried: the next tile's scores between this tile's weights, 962-988; one V buffer and three waves per SIMD, spills, 1134.
-// fp32: 2048 causal tokens 365 us, 94 TFLOP/s (a library product: 154; the matrix units are busy 71 % of a busy unit's time, and tiles of 128 rows
-// compute what the diagonal then masks).
+// fp32: 252 tokens of six users over 4474 earlier ones, 64 heads in groups of eight, 2033 us, 112 TFLOP/s, with a cap 2260; 2048 causal tokens, groups of
+// four, 375 us, 92 (a library product: 154; the matrix units are busy 71 % of a busy unit's time, and tiles of 128 rows compute what the diagonal masks).
 #include "tokens.hpp"
 
 namespace spd {
@@ -387,15 +387,12 @@ __global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
         const char *const kb = k_lds[buf], *const vb = v_lds[buf];
         if (kt < mine.any_hi && kt + BN > mine.any_lo) {  // (some tiles only other waves' rows see)
             f32x16 s[NB];
-            // (pieces are read one ahead of their use; K's in fp32 are not: four products to a piece hide it, and the queries take 64 registers)
+            // (pieces are read one ahead of their use)
             u32x4 kf[2][NB];
-            if (!kF32)
-                read_k(kb, 0, kf[0]);
+            read_k(kb, 0, kf[0]);
 #pragma unroll
             for (int kk = 0; kk < KK; ++kk) {
-                if (kF32)
-                    read_k(kb, kk, kf[kk & 1]);
-                else if (kk + 1 < KK)
+                if (kk + 1 < KK)
                     read_k(kb, kk + 1, kf[(kk + 1) & 1]);
                 multiply_k(kf[kk & 1], kk, s);
                 if constexpr (kF32)
