@@ -58,7 +58,7 @@ typedef __attribute__((address_space(3))) uint32_t lds_u32;
 // for all of them in front of every LDS read that it cannot tell from them.  Nothing but all_loads_done() and a barrier orders reads behind them.
 __device__ __forceinline__ void load_to_lds(const char *from, uint32_t lane_off, uint32_t to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(lane_off), "s"(from) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(lane_off), "s"(from) : "m0", "memory");
 }
 __device__ __forceinline__ uint32_t lds_address(const char *p) { return (uint32_t)uniform((int)(uint32_t)(uintptr_t)(lds_char *)p); }
 __device__ __forceinline__ void all_loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
