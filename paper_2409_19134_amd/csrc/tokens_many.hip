@@ -15,8 +15,8 @@
 // barrier a tile.  16-byte pieces of a row are stored at places xor-ed with the row's number, so that neither
 // the reads of K (16 bytes of eight rows at once) nor the transposed reads of V (32 bytes of four rows) meet in a bank.
 // Masks: a tile that all rows of a wave see whole costs nothing, others are masked element by element, tiles that no row sees are left out.
-// Measured, 32 query heads in groups of four of 128 channels, bf16, results in bf16: 8192 tokens of documents over a cache of 16384 932-970 us, 1.0 PFLOP/s
-// of what the masks leave; 16384 causal tokens 1956-2060 us, 1.07-1.12; 4096 causal tokens 161-170 us, 0.83: two tiles to a place, of which the last to end
+// Measured, 32 query heads in groups of four of 128 channels, bf16, results in bf16: 8192 tokens of documents over a cache of 16384 919-985 us, 1.0 PFLOP/s
+// of what the masks leave; 16384 causal tokens 1938-2060 us, 1.07-1.13; 4096 causal tokens 161-170 us, 0.83: two tiles to a place, of which the last to end
 // leave their neighbours' places empty for 30 us, and 3 us to begin a tile, 3 to end it.  A library product of 8192^3
 // reaches 1.12.  Of the first (966 when it was taken apart) the loads are 118, the exponentials and maxima 104, LDS reads 24; matrix instructions and
 // barriers alone need 673.  Tried: the next tile's scores between this tile's weights, 962-988; one V buffer and three waves per SIMD, spills, 1134.
