@@ -89,7 +89,7 @@ struct TokEntry {
     size_t off_items[host::kTokKernels] = {}, off_joins[host::kTokKernels] = {};
     int64_t n_items[host::kTokKernels] = {}, n_joins[host::kTokKernels] = {}, slots[host::kTokKernels] = {};
     int join_rows[host::kTokKernels] = {}, join_chunks[host::kTokKernels] = {};
-    bool growable = false;
+    bool growable = false, following = false;  // as in TokTables
     // append
     int64_t n_append = 0;
 };
@@ -376,7 +376,7 @@ int find_or_build(ContextBase *ctx, TokensState *t, const spd_shape *s, const sp
         if (!e.valid || e.hash != hash || e.key != t->key)
             continue;
         const int32_t gl = growth(e.lens, t->lens), gq = growth(e.q_pos, t->q_pos);
-        if (gl < 0 || gq < 0 || ((gl || gq) && !e.growable))
+        if (gl < 0 || gq < 0 || ((gl || gq) && !(gl > gq ? e.growable : e.following)))
             continue;
         if (grown && gl + gq >= *grow_len + *grow_q)
             continue;
@@ -425,6 +425,7 @@ int find_or_build(ContextBase *ctx, TokensState *t, const spd_shape *s, const sp
         }
     }
     e->growable = T.growable;
+    e->following = T.following;
     e->key = t->key;
     e->hash = hash;
     e->lens = t->lens;

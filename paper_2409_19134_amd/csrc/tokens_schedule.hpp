@@ -244,7 +244,8 @@ struct TokTables {
     std::vector<TokItem> items[kTokKernels];  // the launch order
     std::vector<TokJoin> joins[kTokKernels];
     int64_t slots[kTokKernels] = {0, 0, 0};
-    bool growable = false;
+    // The tables serve longer lengths and later queries as well, any of them (growable), or where lengths grow by no more than positions (following).
+    bool growable = false, following = false;
     int64_t n_items() const { return (int64_t)(items[0].size() + items[1].size() + items[2].size()); }
 };
 
@@ -321,7 +322,7 @@ inline void build_tok_tables(const spd_shape *s, const spd_kv_view *v, const std
     const int G = s->n_q_heads / s->n_kv_heads, Hkv = s->n_kv_heads, es = elt_size(s->dtype);
     const bool addresses = v->block_size == 0 && !v->k_ptrs_dev;
     T.users.resize(plan.size());
-    T.growable = true;
+    T.growable = T.following = true;
     int32_t tok0 = 0;
     std::vector<TokTile> tiles[kTokKernels];
     std::vector<TokSteps> spans;
@@ -345,12 +346,17 @@ inline void build_tok_tables(const spd_shape *s, const spd_kv_view *v, const std
         if (rows == 0)
             continue;
         const TokKernel k = kernel_for(rows);
-        // A schedule serves longer lengths and later queries as well where a tile's keys end with the view and not with its own causal order.
-        T.growable = T.growable && k != TokKernel::kMany && p.len > 0 && (!causal || p.q_pos + p.n_tok >= p.len) && !(window && !causal);
+        // A schedule serves longer lengths and later queries as well where a tile's keys end with the view and not with its own causal order.  Where
+        // its windows begin behind the view's last key, its keys end with the prefix (or there are none): keys that come into a window
+        // would lie in no stretch, so its lengths may only grow with its positions, windows ahead.
+        T.following = T.following && k != TokKernel::kMany && p.len > 0 && (!causal || p.q_pos + p.n_tok >= p.len) && !(window && !causal);
+        T.growable = T.growable && T.following;
         const int step = k == TokKernel::kMany ? many_keys(s->dtype) : kFewKeys, cap = tile_rows(k);
         for (int64_t r0 = 0; r0 < rows; r0 += cap) {
             const int64_t r1 = std::min<int64_t>(rows, r0 + cap);
-            spans.emplace_back(tile_span(p, causal, window, (int)(r0 / G), (int)((r1 - 1) / G)), step);
+            const TokSpan span = tile_span(p, causal, window, (int)(r0 / G), (int)((r1 - 1) / G));
+            T.growable = T.growable && span.hi == p.len;
+            spans.emplace_back(span, step);
             for (int h = 0; h < Hkv; ++h)
                 tiles[(int)k].push_back(TokTile{(int32_t)u, h, (int32_t)r0, (int32_t)(r1 - r0), spans.back().n, (int32_t)spans.size() - 1});
         }

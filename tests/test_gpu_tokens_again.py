@@ -1,0 +1,69 @@
+"""Calls for several tokens per user that follow other calls of the same context, and what no single call shows, against 64 bits (the tolerances are
+those of test_gpu_tokens.py, whose docstring derives them)."""
+import pytest
+import torch
+
+import token_reference as ref
+from test_gpu_tokens import Problem
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    import paper_2409_19134_amd as spd
+    c = spd.Context(0)
+    yield c
+    torch.cuda.synchronize()
+    c.close()
+
+
+@pytest.mark.parametrize("layout", ["nhd", "paged_hnd16"])
+@pytest.mark.parametrize("window,prefix,new,lens,q_pos", [(32, 0, [1], [64, 104], [104, 104]), (50, 0, [3], [100, 160], [159, 160]),
+                                                          (2, 0, [1], [10, 13], [12, 12]), (8, 5, [2], [40, 60], [60, 60])])
+def test_keys_come_into_a_window_that_lay_behind_them(ctx, layout, window, prefix, new, lens, q_pos):
+    """The other owner's cache is filled piece by piece under queries whose windows begin behind its end at first."""
+    import paper_2409_19134_amd as spd
+    p = Problem((8, 2, 64), "bf16", layout, new, [lens[1]], dict(window=window), "f32", elsewhere=True, seed=2)
+    p.prefix = [prefix] if prefix else None
+    p.store()
+    full_k, full_v, c = p.k, p.v, p.cache
+    for n, at in zip(lens, q_pos):
+        p.held, p.q_pos, p.k, p.v = [n], [at], [full_k[0][:n]], [full_v[0][:n]]
+        if c.page:
+            table = torch.from_numpy(c.table).to(DEV)
+            c.view = spd.KVView(p.held, 64, 16 * 64, k_pool=c.k, v_pool=c.v, block_table=table, block_size=16, block_stride=2 * 16 * 64)
+        else:
+            c.view = spd.KVView(p.held, 2 * 64, 64, k=list(c.k), v=list(c.v))
+        p.score = spd.Score(window=window, prefix=p.prefix, q_pos=p.q_pos)
+        p.check(*p.call(ctx))
+
+
+def test_a_token_step_whose_tokens_move_into_the_prompt(ctx):
+    """One TokenStep with a window: a conversation's turn is generated into the public cache, moved into the prompt's, and the next one begins."""
+    import paper_2409_19134_amd as spd
+    Hq, H, d, dt, window, turn = 8, 2, 64, torch.float32, 32, 40
+    total = 64 + 2 * turn + 3
+    gen = torch.Generator().manual_seed(41)
+    q, k, v = (torch.randn((total, h, d), generator=gen) for h in (Hq, H, H))
+    private, public = ([torch.zeros((n, H, d), device=DEV) for _ in range(2)] for n in (total, turn + 3))
+    for store, rows in zip(private, (k, v)):
+        store[:64] = rows[:64].to(DEV)
+    prompt = spd.KVView([64], H * d, d, k=[private[0]], v=[private[1]])
+    view = spd.KVView([0], H * d, d, k=[public[0]], v=[public[1]])
+    step = spd.TokenStep(ctx, dt, Hq, H, d, 0.125, view, [1], prompt=prompt, window=window)
+    for at in range(64, 64 + 2 * turn):
+        if at == 64 + turn:      # the turn's tokens move
+            for a, b in zip(private, public):
+                a[64:64 + turn] = b[:turn]
+            prompt.lens += turn
+            view.lens -= turn
+        view.lens += 1
+        got, lse = step.run(*(t[at:at + 1].to(DEV) for t in (q, k, v)))
+        torch.cuda.synchronize()
+        a, want, b, most = ref.attend(q[at:at + 1], k[:at + 1], v[:at + 1], ref.visible(1, at + 1, at, 0, True, window), 0.125)
+        # (d + 4) roundings of a score, twice for the two partials' weights, and the 24-bit sums
+        delta = 2 ** -24 * (2 * (d + 4) * most + 256)
+        assert bool(((got.double().cpu() - a).abs() <= (2 * delta + window * 2 ** -24) * b + 1e-6).all()), at
+        assert bool(((lse.double().cpu() - want).abs() <= delta + window * 2 ** -24 + 8 * 2 ** -24 * want.abs()).all()), at

@@ -1,0 +1,33 @@
+"""The host side of the calls for several tokens per user without a GPU: what they launch and upload, recorded by a stand-in HIP runtime and gone through
+key by key and byte by byte (see tests/host/tokens_calls.cpp)."""
+import os
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+
+
+@pytest.fixture(scope="module")
+def program(tmp_path_factory):
+    if not os.path.exists(HIPCC):
+        pytest.skip("hipcc not found")
+    exe = str(tmp_path_factory.mktemp("tokens_calls") / "tokens_calls")
+    cmd = [HIPCC, "--cuda-host-only", "--offload-arch=gfx950", "-O1", "-g", "-std=c++17", "-no-hip-rt", "-rdynamic", "-x", "hip", "-o", exe,
+           os.path.join(ROOT, "tests", "host", "tokens_calls.cpp"), "-ldl"]
+    res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    assert res.returncode == 0, res.stdout[-3000:]
+    return exe
+
+
+def _run(program, *args, **env):
+    lib = os.path.join(ROOT, "paper_2409_19134_amd", "libspd_hip.so")
+    run = subprocess.run([program, lib, *args], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=300, env=dict(os.environ, **env))
+    assert run.returncode == 0 and run.stdout.strip().endswith("ok"), run.stdout[-3000:]
+
+
+def test_tables_used_again_hold_every_key(program):
+    """Lengths and positions that move on from call to call, each by itself: every key that a query sees is in one of the launched stretches, windows that
+    lay behind a cache's last key before it grew among them; a decode loop still builds its table once."""
+    _run(program, "growth")
