@@ -41,7 +41,8 @@ def test_keys_come_into_a_window_that_lay_behind_them(ctx, layout, window, prefi
 
 
 def test_a_token_step_whose_tokens_move_into_the_prompt(ctx):
-    """One TokenStep with a window: a conversation's turn is generated into the public cache, moved into the prompt's, and the next one begins."""
+    """One TokenStep with a window: the last token of a conversation's turn joins the others in the public cache, whose windows lie behind the prompt; the turn is moved
+    into the prompt's cache, and the next one begins."""
     import paper_2409_19134_amd as spd
     Hq, H, d, dt, window, turn = 8, 2, 64, torch.float32, 32, 40
     total = 64 + 2 * turn + 3
@@ -50,10 +51,12 @@ def test_a_token_step_whose_tokens_move_into_the_prompt(ctx):
     private, public = ([torch.zeros((n, H, d), device=DEV) for _ in range(2)] for n in (total, turn + 3))
     for store, rows in zip(private, (k, v)):
         store[:64] = rows[:64].to(DEV)
+    for store, rows in zip(public, (k, v)):
+        store[:turn - 1] = rows[64:64 + turn - 1].to(DEV)
     prompt = spd.KVView([64], H * d, d, k=[private[0]], v=[private[1]])
-    view = spd.KVView([0], H * d, d, k=[public[0]], v=[public[1]])
+    view = spd.KVView([turn - 1], H * d, d, k=[public[0]], v=[public[1]])
     step = spd.TokenStep(ctx, dt, Hq, H, d, 0.125, view, [1], prompt=prompt, window=window)
-    for at in range(64, 64 + 2 * turn):
+    for at in range(64 + turn - 1, 64 + 2 * turn):
         if at == 64 + turn:      # the turn's tokens move
             for a, b in zip(private, public):
                 a[64:64 + turn] = b[:turn]
