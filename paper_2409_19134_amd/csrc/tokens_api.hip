@@ -39,10 +39,9 @@ __global__ __launch_bounds__(256) void tokens_join_kernel(const TokArgs a, const
     for (int c = mine; c < j.n_chunks; c += GROUPS) {
         const float lse2 = a.part_lse[first + (int64_t)c * tile_rows].x;
         const f32x4 v = *reinterpret_cast<const f32x4 *>(a.part_o + (first + (int64_t)c * tile_rows) * D + lane * 4);
-        const float w = fast_exp2(lse2 - m_use);
+        const float w = fast_exp2(lse2 - m_use);  // (a stretch without keys of this row holds zeros; a vanishing weight keeps what is not finite)
         sum += w;
-        if (w != 0.f)
-            o += w * v;
+        o += w * v;
     }
     if constexpr (GROUPS > 1) {
         *reinterpret_cast<f32x4 *>(&part[group][lane * 4]) = o;

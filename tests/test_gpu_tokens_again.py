@@ -70,3 +70,16 @@ def test_a_token_step_whose_tokens_move_into_the_prompt(ctx):
         delta = 2 ** -24 * (2 * (d + 4) * most + 256)
         assert bool(((got.double().cpu() - a).abs() <= (2 * delta + window * 2 ** -24) * b + 1e-6).all()), at
         assert bool(((lse.double().cpu() - want).abs() <= delta + window * 2 ** -24 + 8 * 2 ** -24 * want.abs()).all()), at
+
+
+@pytest.mark.parametrize("dtype,out", [("bf16", "f32"), ("f16", "same"), ("f32", "f32")])
+@pytest.mark.parametrize("new", [[1], [7], [200]])
+def test_far_values_that_are_not_finite_reach_the_queries_that_see_them(ctx, dtype, out, new):
+    """Their weights vanish beside those of the near keys (distance biases over a long cache whose stretches are joined): what is not finite still makes its
+    channel not finite, in the heads that read it, and no others."""
+    p = Problem((8, 2, 64), dtype, "hnd", new, [4000], dict(slopes=True), out, seed=6)
+    p.v[0][5, 0, 1], p.v[0][300, 0, 9], p.v[0][2000, 1, 7] = float("inf"), float("nan"), -float("inf")
+    got, lse = p.store().call(ctx)
+    want = torch.ones(got.shape, dtype=torch.bool)
+    want[:, :4, 1] = want[:, :4, 9] = want[:, 4:, 7] = False
+    assert torch.equal(torch.isfinite(got.cpu()), want) and bool(torch.isfinite(lse).all())
