@@ -10,6 +10,7 @@ struct ContextBase {
     int device = 0;
     int n_cus = 0;
     int last_hip = 0;
+    int cache_entries = 0;                         // views remembered per entry point
     TokensState *tokens = nullptr;                 // made by the first such call
     void (*tokens_free)(TokensState *) = nullptr;  // set with it
 };

@@ -1255,6 +1255,7 @@ int spd_create(spd_ctx **out, int hip_device)
         return SPD_ERR_NOMEM;
     try {
         const int entries = std::min(4096, std::max(1, env_int("SPD_SCHEDULE_CACHE_ENTRIES", kCacheEntriesDefault)));
+        ctx->cache_entries = entries;
         for (auto &own : ctx->owner)
             own.cache.resize((size_t)entries);
     } catch (...) {

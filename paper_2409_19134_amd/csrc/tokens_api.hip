@@ -111,7 +111,7 @@ namespace {
 
 using namespace spd::host;
 
-constexpr size_t kEntries = 128, kSlot = 32 * 1024;
+constexpr size_t kSlot = 32 * 1024;
 
 #define SPD_TRY(ctx, call)                                  \
     do {                                                    \
@@ -179,7 +179,7 @@ TokensState *state_of(ContextBase *ctx)
         TokensState *t = new TokensState();
         try {
             for (auto &list : t->entries)
-                list.resize(kEntries);
+                list.resize((size_t)ctx->cache_entries);
         } catch (...) {
             delete t;
             throw;
@@ -241,11 +241,12 @@ int new_entry(ContextBase *ctx, TokensState *t, int which, size_t bytes, hipStre
         while (cap < bytes)
             cap *= 2;
         free_storage(e);
-        if (cap == kSlot && idx < kEntries) {
+        const size_t slots = (size_t)ctx->cache_entries;
+        if (cap == kSlot && idx < slots) {
             if (!t->slab_dev[which])
-                SPD_TRY(ctx, hipMalloc(reinterpret_cast<void **>(&t->slab_dev[which]), kSlot * kEntries));
+                SPD_TRY(ctx, hipMalloc(reinterpret_cast<void **>(&t->slab_dev[which]), kSlot * slots));
             if (!t->slab_pinned[which])
-                SPD_TRY(ctx, hipHostMalloc(reinterpret_cast<void **>(&t->slab_pinned[which]), kSlot * kEntries, hipHostMallocDefault));
+                SPD_TRY(ctx, hipHostMalloc(reinterpret_cast<void **>(&t->slab_pinned[which]), kSlot * slots, hipHostMallocDefault));
             e.dev = t->slab_dev[which] + idx * kSlot;
             e.pinned = t->slab_pinned[which] + idx * kSlot;
             e.in_slab = true;

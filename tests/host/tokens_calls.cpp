@@ -297,14 +297,42 @@ static void growth()
     }
 }
 
+// As many views are remembered as the context was told to (argument; 0: not told), by each of the calls that remember any.
+static void entries(int told)
+{
+    SYM(spd_append_tokens);
+    spd_ctx *ctx = make();
+    const int n = told ? told : 128, users = 20;  // (an append for few users has no table)
+    for (int which = 0; which < 2; ++which) {
+        auto call = [&](int view) {
+            Attend a(SPD_BF16, 4, 2, 64, std::vector<int32_t>(users, 200), std::vector<int32_t>(users, 1), std::vector<int32_t>(users, 199));
+            a.ptrs[0] = static_cast<const char *>(kNowhere) + 1024 * view;
+            const int before = uploads;
+            if (which == 0 ? a.call(ctx) != SPD_OK
+                           : spd_append_tokens_(ctx, &a.s, &a.v, a.n_new.data(), nullptr, nullptr, nullptr, 0, nullptr, kNowhere, 128, kNowhere, 128, nullptr) != SPD_OK)
+                FAIL("entries: the call fails");
+            return uploads - before;
+        };
+        for (int round = 0; round < 3; ++round)
+            for (int i = 0; i < n; ++i)
+                if (call(i) != (round == 0))
+                    FAIL("call %d, %d views: view %d of round %d", which, n, i, round);
+        if (call(n) != 1 || call(n) != 0 || call(0) != 1)  // one more: the one not used for longest goes
+            FAIL("call %d: more than %d views", which, n);
+    }
+    drop(ctx);
+}
+
 int main(int argc, char **argv)
 {
-    const std::string what = argc == 3 ? argv[2] : "";
-    lib = argc == 3 ? dlopen(argv[1], RTLD_NOW) : nullptr;
+    const std::string what = argc > 2 ? argv[2] : "";
+    lib = argc > 2 ? dlopen(argv[1], RTLD_NOW) : nullptr;
     if (!lib)
-        FAIL("tokens_calls <library> growth");
+        FAIL("tokens_calls <library> growth | entries <number>");
     if (what == "growth")
         growth();
+    else if (what == "entries" && argc == 4)
+        entries(std::atoi(argv[3]));
     else
         FAIL("no such part");
     std::printf("ok\n");

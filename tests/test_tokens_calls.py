@@ -31,3 +31,9 @@ def test_tables_used_again_hold_every_key(program):
     """Lengths and positions that move on from call to call, each by itself: every key that a query sees is in one of the launched stretches, windows that
     lay behind a cache's last key before it grew among them; a decode loop still builds its table once."""
     _run(program, "growth")
+
+
+@pytest.mark.parametrize("told", [0, 1, 5, 300])
+def test_as_many_views_as_the_context_was_told_to_remember(program, told):
+    """SPD_SCHEDULE_CACHE_ENTRIES, which spd_create reads, holds for these calls too: so many views build their tables once, one more takes a place."""
+    _run(program, "entries", str(told), **({"SPD_SCHEDULE_CACHE_ENTRIES": str(told)} if told else {}))
