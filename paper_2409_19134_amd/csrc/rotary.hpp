@@ -26,6 +26,7 @@ struct RotateArgs {
     int64_t x_stride, y_stride;  // bytes between tokens
     int32_t n_heads;
     int32_t per_group;           // tokens of a workgroup, up to kTurnTokens
+    int32_t first;               // the launch's first token
 };
 
 // New tokens of one user that lie next to each other: up to kTurnTokens of them.
@@ -188,7 +189,7 @@ __global__ __launch_bounds__(256) void rotate_kernel(const RotateArgs a)
 {
     typedef TurnPlace<DT, D, ADJACENT> Place;
     __shared__ float2 cs[kTurnTokens][64];
-    const int token0 = blockIdx.x * a.per_group, count = min(a.per_group, a.turn.n_tokens - token0);
+    const int token0 = a.first + (int)blockIdx.x * a.per_group, count = min(a.per_group, a.turn.n_tokens - token0);
     fill_turns(cs, a.turn, token0, count);
     __syncthreads();
     const int places = turn_places(Place::ES, D, ADJACENT, a.turn.n_pairs), step = 256 / places;

@@ -111,6 +111,16 @@ namespace {
 
 using namespace spd::host;
 
+// A launch takes fewer than 2^32 threads to a dimension: calls of more workgroups (tens of millions of tokens, or of users' heads) go in parts, each
+// launch(first, count).  (A multiple of eight: the XCD that a workgroup runs on stays its number's.)
+constexpr int64_t kMostGroups = (int64_t)1 << 23;
+template <class F>
+void in_parts(int64_t groups, F &&launch)
+{
+    for (int64_t first = 0; first < groups; first += kMostGroups)
+        launch(first, (unsigned)std::min(groups - first, kMostGroups));
+}
+
 constexpr size_t kSlot = 32 * 1024;
 
 #define SPD_TRY(ctx, call)                                  \
@@ -554,23 +564,28 @@ int attend(ContextBase *ctx, const spd_shape *s, const void *q, int64_t q_stride
         if (e->n_items[k] == 0)
             continue;
         const int cap = tile_rows((TokKernel)k);
-        a.items = reinterpret_cast<const TokItem *>(e->dev + e->off_items[k]);
+        const TokItem *const items = reinterpret_cast<const TokItem *>(e->dev + e->off_items[k]);
         a.part_o = t->part + rows[k] * (size_t)s->head_dim;
         a.part_lse = part_lse + rows[k];
-        if (k == (int)TokKernel::kMany)
-            launch_tokens_many(s->dtype, s->head_dim, modified, e->n_items[k], a, stream);
-        else
-            launch_tokens_few(s->dtype, s->head_dim, paged, cap, modified, e->n_items[k], a, stream);
+        in_parts(e->n_items[k], [&](int64_t first, unsigned n) {
+            a.items = items + first;
+            if (k == (int)TokKernel::kMany)
+                launch_tokens_many(s->dtype, s->head_dim, modified, n, a, stream);
+            else
+                launch_tokens_few(s->dtype, s->head_dim, paged, cap, modified, n, a, stream);
+        });
         SPD_TRY(ctx, hipGetLastError());
         if (e->n_joins[k] == 0)
             continue;
         const TokJoin *joins = reinterpret_cast<const TokJoin *>(e->dev + e->off_joins[k]);
-        if (s->dtype == SPD_F32)
-            launch_join<SPD_F32>(s->head_dim, e->n_joins[k], e->join_rows[k], e->join_chunks[k], a, joins, cap, stream);
-        else if (s->dtype == SPD_BF16)
-            launch_join<SPD_BF16>(s->head_dim, e->n_joins[k], e->join_rows[k], e->join_chunks[k], a, joins, cap, stream);
-        else
-            launch_join<SPD_F16>(s->head_dim, e->n_joins[k], e->join_rows[k], e->join_chunks[k], a, joins, cap, stream);
+        in_parts(e->n_joins[k], [&](int64_t first, unsigned n) {
+            if (s->dtype == SPD_F32)
+                launch_join<SPD_F32>(s->head_dim, n, e->join_rows[k], e->join_chunks[k], a, joins + first, cap, stream);
+            else if (s->dtype == SPD_BF16)
+                launch_join<SPD_BF16>(s->head_dim, n, e->join_rows[k], e->join_chunks[k], a, joins + first, cap, stream);
+            else
+                launch_join<SPD_F16>(s->head_dim, n, e->join_rows[k], e->join_chunks[k], a, joins + first, cap, stream);
+        });
         SPD_TRY(ctx, hipGetLastError());
     }
     return SPD_OK;
@@ -703,6 +718,7 @@ int append(ContextBase *ctx, const spd_shape *s, const spd_kv_view *v, const int
             }
     };
     AppendItems given;
+    const AppendItem *items = nullptr;
     if (n_items <= kAppendByValue) {
         fill(given.it);
         a.by_value = 1;
@@ -738,11 +754,14 @@ int append(ContextBase *ctx, const spd_shape *s, const spd_kv_view *v, const int
         }
         if (rc != SPD_OK)
             return rc;
-        a.items = reinterpret_cast<const AppendItem *>(e->dev);
+        items = reinterpret_cast<const AppendItem *>(e->dev);
     }
     const bool once = total * token_bytes >= kOnceBytes;
     with_turn_kernel(s->dtype, s->head_dim, rope && rope->adjacent, once, [&](auto dt, auto d, auto adjacent, auto once) {
-        hipLaunchKernelGGL((append_kernel<dt(), d(), adjacent(), once()>), dim3((unsigned)n_items), dim3(256), 0, stream, a, given);
+        in_parts(n_items, [&](int64_t first, unsigned n) {
+            a.items = items ? items + first : nullptr;
+            hipLaunchKernelGGL((append_kernel<dt(), d(), adjacent(), once()>), dim3(n), dim3(256), 0, stream, a, given);
+        });
     });
     SPD_TRY(ctx, hipGetLastError());
     return SPD_OK;
@@ -796,10 +815,13 @@ int spd_rotate(spd_ctx *ctx, int32_t dtype, int32_t head_dim, const spd_rope *ro
     a.n_heads = n_heads;
     const int64_t token_bytes = (int64_t)n_heads * head_dim * es;
     a.per_group = tokens_per_group(n_tokens, token_bytes, c->n_cus);
-    const unsigned blocks = (unsigned)(((int64_t)n_tokens + a.per_group - 1) / a.per_group);
+    const int64_t groups = ((int64_t)n_tokens + a.per_group - 1) / a.per_group;
     const bool once = n_tokens * token_bytes >= kOnceBytes;
     with_turn_kernel(dtype, head_dim, rope->adjacent != 0, once, [&](auto dt, auto d, auto adjacent, auto once) {
-        hipLaunchKernelGGL((rotate_kernel<dt(), d(), adjacent(), once()>), dim3(blocks), dim3(256), 0, static_cast<hipStream_t>(hip_stream), a);
+        in_parts(groups, [&](int64_t first, unsigned n) {
+            a.first = (int32_t)(first * a.per_group);
+            hipLaunchKernelGGL((rotate_kernel<dt(), d(), adjacent(), once()>), dim3(n), dim3(256), 0, static_cast<hipStream_t>(hip_stream), a);
+        });
     });
     SPD_TRY(c, hipGetLastError());
     return SPD_OK;

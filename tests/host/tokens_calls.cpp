@@ -9,6 +9,7 @@
 #include <map>
 #include <random>
 #include <string>
+#include <utility>
 #include <vector>
 
 #include "../../paper_2409_19134_amd/csrc/rotary.hpp"
@@ -22,9 +23,12 @@ struct Launch {
     dim3 grid, block;
     TokArgs attend;      // the attention's kernels and the join
     const TokJoin *joins;
+    RotateArgs rotate;
+    AppendArgs append;
 };
 static std::vector<Launch> launches;
 static int uploads = 0;
+static hipError_t last_error = hipSuccess;
 static hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
 
 static std::map<const void *, std::string> &names()
@@ -56,7 +60,7 @@ hipError_t hipEventCreateWithFlags(hipEvent_t *e, unsigned) { return *e = (hipEv
 hipError_t hipEventDestroy(hipEvent_t) { return hipSuccess; }
 hipError_t hipEventRecord(hipEvent_t, hipStream_t) { return hipSuccess; }
 hipError_t hipEventSynchronize(hipEvent_t) { return hipSuccess; }
-hipError_t hipGetLastError() { return hipSuccess; }
+hipError_t hipGetLastError() { return std::exchange(last_error, hipSuccess); }
 hipError_t hipStreamIsCapturing(hipStream_t, hipStreamCaptureStatus *status) { return *status = capture, hipSuccess; }
 void **__hipRegisterFatBinary(const void *)
 {
@@ -78,7 +82,10 @@ hipError_t __hipPopCallConfiguration(dim3 *grid, dim3 *block, size_t *lds, hipSt
 }
 hipError_t hipLaunchKernel(const void *fn, dim3 grid, dim3 block, void **args, size_t, hipStream_t)
 {
-    Launch l = {names()[fn], grid, block, {}, nullptr};
+    Launch l = {names()[fn], grid, block, {}, nullptr, {}, {}};
+    for (uint64_t threads : {(uint64_t)grid.x * block.x, (uint64_t)grid.y * block.y, (uint64_t)grid.z * block.z})
+        if (threads == 0 || threads > 0xffffffffull)  // the runtime's limit for each dimension
+            return last_error = hipErrorInvalidConfiguration;
     if (l.kernel.find("tokens_upload_kernel") != std::string::npos) {
         std::memcpy(*static_cast<char **>(args[1]), *static_cast<const char **>(args[0]), (size_t)*static_cast<unsigned *>(args[2]) * 16);
         ++uploads;
@@ -86,6 +93,10 @@ hipError_t hipLaunchKernel(const void *fn, dim3 grid, dim3 block, void **args, s
     }
     if (l.kernel.find("tokens_") != std::string::npos)
         std::memcpy(&l.attend, args[0], sizeof l.attend);
+    if (l.kernel.find("rotate_kernel") != std::string::npos)
+        std::memcpy(&l.rotate, args[0], sizeof l.rotate);
+    if (l.kernel.find("append_kernel") != std::string::npos)
+        std::memcpy(&l.append, args[0], sizeof l.append);
     if (l.kernel.find("tokens_join_kernel") != std::string::npos)
         l.joins = *static_cast<const TokJoin **>(args[1]);
     launches.push_back(l);
@@ -323,14 +334,78 @@ static void entries(int told)
     drop(ctx);
 }
 
+// Calls of so many workgroups that one launch would pass the runtime's limit of 2^32 threads to a dimension: they go through, and take everything once.
+static void limits()
+{
+    SYM(spd_rotate);
+    SYM(spd_append_tokens);
+    spd_ctx *ctx = make();
+    spd_rope rope = {1, 32, 0, nullptr, static_cast<const float *>(kNowhere), 1.f};
+    struct Case {
+        int32_t tokens, heads;
+    };
+    for (const Case &c : {Case{(1 << 26) + 5, 1}, Case{0x7fffffff, 2}, Case{(1 << 24) + 3, 64}, Case{1 << 23, 100}, Case{1000, 3}}) {
+        launches.clear();
+        const int rc = spd_rotate_(ctx, SPD_BF16, 64, &rope, c.tokens, static_cast<const int32_t *>(kNowhere), c.heads, kNowhere, 64 * c.heads, kNowhere, 64 * c.heads, 0, nullptr);
+        if (rc != SPD_OK)
+            FAIL("rotation of %d tokens of %d heads: %d", c.tokens, c.heads, rc);
+        int64_t next = 0;
+        for (const Launch &l : launches) {
+            const RotateArgs &a = l.rotate;
+            if (a.first != next || a.turn.n_tokens != c.tokens || a.per_group < 1 || a.per_group > kTurnTokens)
+                FAIL("rotation of %d tokens: a launch from %d, %lld were taken", c.tokens, a.first, (long long)next);
+            next += (int64_t)l.grid.x * a.per_group;
+        }
+        if (next < c.tokens || next - c.tokens >= launches.back().rotate.per_group)
+            FAIL("rotation of %d tokens: %lld are taken", c.tokens, (long long)next);
+    }
+    {
+        const int32_t tokens = (1 << 26) + 9;
+        Attend a(SPD_BF16, 1, 1, 64, {tokens + 7}, {tokens}, {0});
+        launches.clear();
+        const int rc = spd_append_tokens_(ctx, &a.s, &a.v, a.n_new.data(), nullptr, nullptr, nullptr, 0, nullptr, kNowhere, 64, kNowhere, 64, nullptr);
+        if (rc != SPD_OK)
+            FAIL("append of %d tokens: %d", tokens, rc);
+        int64_t next = 0;
+        for (const Launch &l : launches)
+            for (unsigned i = 0; i < l.grid.x; ++i) {
+                const AppendItem &it = l.append.items[i];
+                if (it.token != next || it.place + l.append.grow != next + 7 || it.count < 1 || it.count > kTurnTokens)
+                    FAIL("append of %d tokens: %d tokens from %d at %d, %lld were taken", tokens, it.count, it.token, it.place + l.append.grow, (long long)next);
+                next += it.count;
+            }
+        if (next != tokens)
+            FAIL("append of %d tokens: %lld are taken", tokens, (long long)next);
+    }
+    {
+        const int users = (1 << 18) + 1, heads = 64;
+        Attend a(SPD_BF16, heads, heads, 64, std::vector<int32_t>(users, 1), std::vector<int32_t>(users, 1), std::vector<int32_t>(users, 0));
+        if (const int rc = a.call(ctx); rc != SPD_OK)
+            FAIL("attention of %d users: %d", users, rc);
+        std::vector<char> seen((size_t)users * heads, 0);
+        for (const Launch &l : launches)
+            for (unsigned i = 0; i < l.grid.x; ++i) {
+                const TokItem &it = l.attend.items[i];
+                if (it.n_rows != 1 || seen[(size_t)it.user * heads + (size_t)it.kv_head]++)
+                    FAIL("attention of %d users: user %d head %d is taken twice", users, it.user, it.kv_head);
+            }
+        for (char x : seen)
+            if (!x)
+                FAIL("attention of %d users: a row is not taken", users);
+    }
+    drop(ctx);
+}
+
 int main(int argc, char **argv)
 {
     const std::string what = argc > 2 ? argv[2] : "";
     lib = argc > 2 ? dlopen(argv[1], RTLD_NOW) : nullptr;
     if (!lib)
-        FAIL("tokens_calls <library> growth | entries <number>");
+        FAIL("tokens_calls <library> growth | limits | entries <number>");
     if (what == "growth")
         growth();
+    else if (what == "limits")
+        limits();
     else if (what == "entries" && argc == 4)
         entries(std::atoi(argv[3]));
     else

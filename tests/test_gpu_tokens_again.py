@@ -83,3 +83,29 @@ def test_far_values_that_are_not_finite_reach_the_queries_that_see_them(ctx, dty
     want = torch.ones(got.shape, dtype=torch.bool)
     want[:, :4, 1] = want[:, :4, 9] = want[:, 4:, 7] = False
     assert torch.equal(torch.isfinite(got.cpu()), want) and bool(torch.isfinite(lse).all())
+
+
+def test_rotation_and_append_of_more_tokens_than_a_launch_takes(ctx):
+    """2^26 tokens and a few more: what a call for the tokens around the launches' borders and at the end computes, bit by bit, and every other token copied or
+    turned as well."""
+    import paper_2409_19134_amd as spd
+    T, d = (1 << 26) + 5, 64
+    x = torch.empty((T, 1, d), dtype=torch.bfloat16, device=DEV)
+    for at in range(0, T, 1 << 23):
+        x[at:at + (1 << 23)].normal_()
+    pos = torch.arange(T, dtype=torch.int32, device=DEV)
+    rope = spd.Rope(torch.linspace(1.0, 0.001, 32, device=DEV))
+    y = ctx.spd_rotate(rope, x, pos)
+    for at in range(0, T, 1 << 23):
+        piece = slice(at, min(T, at + (1 << 23)))
+        assert torch.equal(y[piece], ctx.spd_rotate(rope, x[piece], pos[piece])), at
+    k = torch.zeros(((T + 9) * d,), dtype=torch.bfloat16, device=DEV)
+    v = torch.zeros_like(k)
+    view = spd.KVView([T + 2], d, d, k=[k], v=[v])
+    ctx.spd_append_tokens(spd.make_shape(torch.bfloat16, 1, 1, d, 1.0), view, [T], x, y)
+    for store, rows in ((k, x), (v, y)):
+        store = store.view(T + 9, d)
+        assert bool((store[:2] == 0).all()) and bool((store[T + 2:] == 0).all())
+        for at in range(0, T, 1 << 23):
+            piece = rows[at:at + (1 << 23), 0]
+            assert torch.equal(store[2 + at:2 + at + piece.shape[0]], piece), at

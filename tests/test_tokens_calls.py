@@ -37,3 +37,8 @@ def test_tables_used_again_hold_every_key(program):
 def test_as_many_views_as_the_context_was_told_to_remember(program, told):
     """SPD_SCHEDULE_CACHE_ENTRIES, which spd_create reads, holds for these calls too: so many views build their tables once, one more takes a place."""
     _run(program, "entries", str(told), **({"SPD_SCHEDULE_CACHE_ENTRIES": str(told)} if told else {}))
+
+
+def test_calls_of_more_workgroups_than_a_launch_takes(program):
+    """Tens of millions of tokens in one rotation or append, of (user, head) pairs in one attention: every one is taken once."""
+    _run(program, "limits")
