@@ -25,6 +25,7 @@ struct Launch {
     const TokJoin *joins;
     RotateArgs rotate;
     AppendArgs append;
+    AppendItems given;
 };
 static std::vector<Launch> launches;
 static int uploads = 0;
@@ -82,7 +83,7 @@ hipError_t __hipPopCallConfiguration(dim3 *grid, dim3 *block, size_t *lds, hipSt
 }
 hipError_t hipLaunchKernel(const void *fn, dim3 grid, dim3 block, void **args, size_t, hipStream_t)
 {
-    Launch l = {names()[fn], grid, block, {}, nullptr, {}, {}};
+    Launch l = {names()[fn], grid, block, {}, nullptr, {}, {}, {}};
     for (uint64_t threads : {(uint64_t)grid.x * block.x, (uint64_t)grid.y * block.y, (uint64_t)grid.z * block.z})
         if (threads == 0 || threads > 0xffffffffull)  // the runtime's limit for each dimension
             return last_error = hipErrorInvalidConfiguration;
@@ -95,8 +96,10 @@ hipError_t hipLaunchKernel(const void *fn, dim3 grid, dim3 block, void **args, s
         std::memcpy(&l.attend, args[0], sizeof l.attend);
     if (l.kernel.find("rotate_kernel") != std::string::npos)
         std::memcpy(&l.rotate, args[0], sizeof l.rotate);
-    if (l.kernel.find("append_kernel") != std::string::npos)
+    if (l.kernel.find("append_kernel") != std::string::npos) {
         std::memcpy(&l.append, args[0], sizeof l.append);
+        std::memcpy(&l.given, args[1], sizeof l.given);
+    }
     if (l.kernel.find("tokens_join_kernel") != std::string::npos)
         l.joins = *static_cast<const TokJoin **>(args[1]);
     launches.push_back(l);
@@ -334,6 +337,74 @@ static void entries(int told)
     drop(ctx);
 }
 
+// Append tables that are used again after the lengths have moved on: every new token goes to its place, and a loop in which all users move on alike
+// builds its table once.
+static void append()
+{
+    SYM(spd_append_tokens);
+    std::mt19937 rng(9);
+    auto pick = [&](int lo, int hi) { return lo + (int)(rng() % (unsigned)(hi - lo + 1)); };
+    for (int round = 0; round < 60; ++round) {
+        spd_ctx *ctx = make();
+        const int users = pick(1, 60), mode = round % 4;  // contiguous, a head stride for each user, device pointer tables, pages
+        std::vector<int32_t> lens, n_new;
+        std::vector<int64_t> head_strides;
+        for (int u = 0; u < users; ++u) {
+            n_new.push_back(pick(0, 3) ? pick(0, 9) : 0);
+            lens.push_back(n_new.back() + pick(0, 200));
+            head_strides.push_back(64 * pick(300, 2000));
+        }
+        Attend a(SPD_F16, 4, 2, 64, lens, n_new, std::vector<int32_t>((size_t)users, 0));
+        for (int u = 0; u < users; ++u)
+            a.ptrs[(size_t)u] = static_cast<const char *>(kNowhere) + ((int64_t)u << 30);
+        if (mode == 1)
+            a.v.head_strides = head_strides.data();
+        if (mode == 2)
+            a.v.k_ptrs_dev = a.v.v_ptrs_dev = a.ptrs.data();
+        if (mode == 3) {
+            a.v.block_size = 16;
+            a.v.k_pool = a.v.v_pool = kNowhere;
+            a.v.block_table = static_cast<const int32_t *>(kNowhere);
+            a.v.max_blocks = 100;
+            a.v.block_stride = 2 * 16 * 64;
+        }
+        bool alike = false;
+        for (int step = 0; step < 20; ++step) {
+            const int before = uploads;
+            launches.clear();
+            if (spd_append_tokens_(ctx, &a.s, &a.v, a.n_new.data(), nullptr, nullptr, nullptr, 0, nullptr, kNowhere, 128, kNowhere, 128, nullptr) != SPD_OK)
+                FAIL("append: the call fails");
+            if (alike && uploads != before)
+                FAIL("append: step %d builds its table again", step);
+            int32_t token = 0, user = 0, taken = 0;
+            for (const Launch &l : launches)
+                for (unsigned i = 0; i < l.grid.x; ++i) {
+                    const AppendItem &it = l.append.by_value ? l.given.it[i] : l.append.items[i];
+                    while (taken == a.n_new[(size_t)user])
+                        ++user, taken = 0;
+                    const void *base = l.append.k_pool ? nullptr : l.append.k_ptrs ? l.append.k_ptrs[user] : it.k_base;
+                    if (it.user != user || it.token != token || it.count < 1 || it.count > a.n_new[(size_t)user] - taken ||
+                        it.place + l.append.grow != a.lens[(size_t)user] - a.n_new[(size_t)user] + taken || (!l.append.k_pool && base != a.ptrs[(size_t)user]) ||
+                        it.head_stride != 2 * (mode == 1 ? head_strides[(size_t)user] : a.v.head_stride))
+                        FAIL("append: step %d: user %d token %d goes to user %d, %d tokens at %d", step, user, token, it.user, it.count, it.place + l.append.grow);
+                    taken += it.count;
+                    token += it.count;
+                }
+            for (int n : a.n_new)
+                token -= n;
+            if (token != 0)
+                FAIL("append: step %d: not every token is taken", step);
+            alike = pick(0, 2) != 0;
+            const int all = pick(0, 40);
+            for (int32_t &l : a.lens)
+                l += all;
+            if (!alike)
+                a.lens[(size_t)pick(0, users - 1)] += pick(1, 20);
+        }
+        drop(ctx);
+    }
+}
+
 // Calls of so many workgroups that one launch would pass the runtime's limit of 2^32 threads to a dimension: they go through, and take everything once.
 static void limits()
 {
@@ -401,11 +472,13 @@ int main(int argc, char **argv)
     const std::string what = argc > 2 ? argv[2] : "";
     lib = argc > 2 ? dlopen(argv[1], RTLD_NOW) : nullptr;
     if (!lib)
-        FAIL("tokens_calls <library> growth | limits | entries <number>");
+        FAIL("tokens_calls <library> growth | append | limits | entries <number>");
     if (what == "growth")
         growth();
     else if (what == "limits")
         limits();
+    else if (what == "append")
+        append();
     else if (what == "entries" && argc == 4)
         entries(std::atoi(argv[3]));
     else

@@ -109,3 +109,35 @@ def test_rotation_and_append_of_more_tokens_than_a_launch_takes(ctx):
         for at in range(0, T, 1 << 23):
             piece = rows[at:at + (1 << 23), 0]
             assert torch.equal(store[2 + at:2 + at + piece.shape[0]], piece), at
+
+
+@pytest.mark.parametrize("layout", ["nhd", "hnd", "tables", "paged_hnd16", "paged_nhd64"])
+def test_append_tables_used_again(ctx, layout):
+    """A call for forty users (its table on the device), some without new tokens, again and again: all lengths move on by one, by a page, then one user's alone.
+    After every call the new rows are in their places and nothing else has changed."""
+    import paper_2409_19134_amd as spd
+    H, d, dt = 2, 64, torch.float16
+    gen = torch.Generator().manual_seed(43)
+    new = [(0, 1, 3, 1, 2)[u % 5] for u in range(40)]
+    held = [n + u % 23 for u, n in enumerate(new)]
+    most = [l + 130 for l in held]
+    rows = [[torch.randn((l, H, d), generator=gen).to(dt) for l in most] for _ in range(2)]
+    cache = ref.Cache(spd, *rows, layout, DEV, seed=4)
+    want = [x.clone() for x in (cache.k, cache.v)]
+    where = ref.Cache.__new__(ref.Cache)
+    where.__dict__.update(cache.__dict__, k=want[0], v=want[1])
+    shape, T = spd.make_shape(dt, H, H, d, 1.0), sum(new)
+    for move in (0, 1, 1, 16, 64, None, 1):
+        if move is None:
+            held[7] += 5
+        else:
+            held = [l + move for l in held]
+        cache.view.lens[:] = held
+        k_new, v_new = (torch.randn((T, H, d), generator=gen).to(dt) for _ in range(2))
+        ctx.spd_append_tokens(shape, cache.view, new, k_new.to(DEV), v_new.to(DEV))
+        at = 0
+        for u, n in enumerate(new):
+            where.put(u, held[u] - n, k_new[at:at + n], v_new[at:at + n])
+            at += n
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(cache.bits(), where.bits())), move

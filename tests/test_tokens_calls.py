@@ -33,6 +33,11 @@ def test_tables_used_again_hold_every_key(program):
     _run(program, "growth")
 
 
+def test_append_tables_used_again(program):
+    """Users' lengths that move on alike (the table is used again) or by themselves, in every kind of storage: every new token goes to its place."""
+    _run(program, "append")
+
+
 @pytest.mark.parametrize("told", [0, 1, 5, 300])
 def test_as_many_views_as_the_context_was_told_to_remember(program, told):
     """SPD_SCHEDULE_CACHE_ENTRIES, which spd_create reads, holds for these calls too: so many views build their tables once, one more takes a place."""
