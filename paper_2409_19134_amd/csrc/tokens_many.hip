@@ -56,9 +56,10 @@ typedef __attribute__((address_space(3))) uint32_t lds_u32;
 
 // Sixteen bytes from every lane's offset behind `from` to its place behind `to` (both the wave's) without a trip through registers.  Not by the builtin: the compiler then waits
 // for all of them in front of every LDS read that it cannot tell from them.  Nothing but all_loads_done() and a barrier orders reads behind them.
+// `to` travels in M0, as an operand: the compiler writes that register and knows when (the wait state behind the write is the asm's).
 __device__ __forceinline__ void load_to_lds(const char *from, uint32_t lane_off, uint32_t to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(lane_off), "s"(from) : "m0", "memory");
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"{m0}"(to), "v"(lane_off), "s"(from) : "memory");
 }
 __device__ __forceinline__ uint32_t lds_address(const char *p) { return (uint32_t)uniform((int)(uint32_t)(uintptr_t)(lds_char *)p); }
 __device__ __forceinline__ void all_loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
