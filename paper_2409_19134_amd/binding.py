@@ -176,6 +176,7 @@ class KVView:
         self.lens = np.ascontiguousarray(lens, dtype=np.int32)
         n = int(self.lens.shape[0])
         self._keep = (k, v, k_pool, v_pool, block_table)
+        self.devices = {t.get_device() for t in (*(k or ()), *(v or ()), k_pool, v_pool, block_table) if t is not None and t.numel()}
         st = spd_kv_view()
         st.n_users = n
         st.lens = self.lens.ctypes.data_as(C.POINTER(C.c_int32))
@@ -324,8 +325,9 @@ class Context:
         except Exception:
             pass
 
-    def _here(self, *tensors):
-        """The tensors lie on the context's device (a kernel must not follow other addresses)."""
+    def _here(self, view: Optional[KVView], *tensors):
+        """The view's caches and the tensors lie on the context's device (a kernel must not follow other addresses)."""
+        assert view is None or view.devices <= {self.device}
         for t in tensors:
             assert t is None or t.get_device() == self.device
 
@@ -522,7 +524,7 @@ class Context:
         if y is None:
             y = torch.empty((T, H, d), device=x.device, dtype=x.dtype)
         assert y.dtype == x.dtype
-        self._here(x, y, positions, rope.inv_freq)
+        self._here(None, x, y, positions, rope.inv_freq)
         assert positions.dtype is torch.int32 and positions.is_contiguous() and positions.numel() == rope.struct.n_axes * T
         rc = lib.spd_rotate(self.handle, _DTYPE_CODES[x.dtype], d, C.byref(rope.struct), T, positions.data_ptr(), H, x.data_ptr(),
                             _token_rows(x, T, H, d), y.data_ptr(), _token_rows(y, T, H, d), int(bool(transposed)), _stream_ptr(stream, self.device))
@@ -537,9 +539,9 @@ class Context:
         Hq, H, d, dtype = shape.n_q_heads, shape.n_kv_heads, shape.head_dim, _CODE_DTYPES[shape.dtype]
         ks, vs, qs = _token_rows(k_new, T, H, d), _token_rows(v_new, T, H, d), 0
         assert k_new.dtype == v_new.dtype == dtype
-        self._here(k_new, v_new, q, q_out if q is not None else None)
+        self._here(view, k_new, v_new, q, q_out if q is not None else None)
         if rope is not None:
-            self._here(positions, rope.inv_freq)
+            self._here(None, positions, rope.inv_freq)
         assert rope is None or (positions.dtype is torch.int32 and positions.is_contiguous() and positions.numel() == rope.struct.n_axes * T)
         if q is not None:
             qs = _token_rows(q, T, Hq, d)
@@ -566,10 +568,10 @@ class Context:
         qs = _token_rows(q, T, Hq, d)
         assert q.dtype == dtype and out.is_contiguous() and out.shape == (T, Hq, d) and out.dtype in (torch.float32, dtype)
         assert lse.is_contiguous() and lse.shape == (T, Hq) and lse.dtype is torch.float32
-        self._here(q, out, lse)
+        self._here(view, q, out, lse)
         if score is not None:
             score.check(view.struct.n_users, T, Hq)
-            self._here(score.slopes, score.ranges)
+            self._here(None, score.slopes, score.ranges)
         rc = lib.spd_partial_attn_tokens(self.handle, C.byref(shape), q.data_ptr(), qs, C.byref(view.struct), _address(counts),
                                          None if score is None else C.byref(score.struct), out.data_ptr(), _DTYPE_CODES[out.dtype],
                                          lse.data_ptr(), _stream_ptr(stream, self.device))
