@@ -353,7 +353,7 @@ int spd_build_schedule(const spd_shape *shape, int32_t n_users, const int32_t *l
  * Several new tokens per user: a prompt, a chunk of one, tokens proposed for checking, or one token each with scores
  * that are more than scaled products.  What is written into a cache (rotated keys, values) and the partial attention
  * that reads it.  Token arrays hold the users' new tokens one user after the other, n_new[u] of user u (ragged;
- * T = sum of n_new).  Everything said at the top of this file holds; unlike the calls above these leave the calling
+ * T = sum of n_new).  Everything said at the top of this file holds, but for results that are asked for in 16 bits; unlike the calls above these leave the calling
  * thread's current HIP device as it was.  A view's `lens` already count the new tokens: user u's are the last n_new[u]
  * of its lens[u] tokens.
  */
@@ -420,7 +420,7 @@ int spd_append_tokens(spd_ctx *ctx, const spd_shape *shape, const spd_kv_view *v
  */
 typedef struct spd_score {
     float cap;              /* 0 (none) or positive, at most 1e30, scale / cap neither subnormal nor near overflow  */
-    const float *slopes;    /* DEVICE [Hq] finite, or NULL                                                          */
+    const float *slopes;    /* DEVICE [Hq], finite also times the longest distance, or NULL                          */
     int32_t causal;         /* 0 or 1                                                                               */
     int32_t window;         /* 0: unlimited, else 1 .. 2^30                                                         */
     const int32_t *prefix;  /* HOST [n_users], 0 .. 2^30, or NULL: none                                             */
@@ -437,9 +437,12 @@ typedef struct spd_score {
  *   n_new      HOST [n_users], 0 .. 2^30 (at most lens[u] where q_pos is NULL); T * Hq at most 2^31 - 1
  *   view       as in the partial calls; token_stride and, paged, block_stride at most 2^28 bytes
  *   q          DEVICE [T][Hq][d], the tokens q_token_stride elements apart (as in spd_append_tokens)
- *   out        DEVICE [T][Hq][d] of out_dtype: SPD_F32, or shape->dtype (each value rounded once; 16-bit probabilities
- *              then enter the second product rounded once too)
- *   lse        DEVICE [T][Hq] fp32
+ *   out        DEVICE [T][Hq][d] of out_dtype: SPD_F32, or shape->dtype, to which each value is then rounded.  Probabilities
+ *              exp(s_k - lse) enter the second product in 24 bits (fp16: 22).  Not so for 16-bit results of users with more than
+ *              32 rows (n_new[u] * Hq / Hkv): theirs are rounded to shape->dtype there (8 bits in bf16, 11 in fp16), beside the
+ *              result's own rounding an error of up to half a step of that type of sum_k p_k |v_k|.
+ *   lse        DEVICE [T][Hq] fp32.  Where out is of 16 bits, a user has more than 32 rows, there are no slopes and 0 < cap <= 64, it
+ *              may be off by cap * 2^-20 (the cap's tanh is then formed in 22 bits); elsewhere by what 24-bit sums of the scores leave.
  *   score      NULL: all zero
  * Few rows over long caches are split over the keys and joined; many go through matrix tiles.  The same graph rules as
  * for the partial calls above: run a call once eagerly before it is recorded (a call that has to build its schedule or

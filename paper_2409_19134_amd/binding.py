@@ -519,7 +519,7 @@ class Context:
     def spd_rotate(self, rope: Rope, x: torch.Tensor, positions: torch.Tensor, y: Optional[torch.Tensor] = None, transposed: bool = False,
                    stream=None):
         """Rotary positions on x [T][heads][d] (heads end to end; tokens may be further apart) into y (default: a new tensor; x itself turns
-        in place).  positions: int32 [axes][T] (or [T] with one axis)."""
+        in place).  positions: int32 [axes][T] (or [T] with one axis).  No gradient is recorded: `transposed` turns y's into x's."""
         T, H, d = x.shape
         if y is None:
             y = torch.empty((T, H, d), device=x.device, dtype=x.dtype)

@@ -2,7 +2,8 @@
 //
 // A workgroup takes a few tokens.  It first forms their cosines and sines, one (token, pair) to a thread, into LDS: the heads of a token
 // share them.  Then every thread keeps one place of a head - sixteen bytes and, for pairs half a rotation apart, the sixteen that turn with
-// them - and goes through all heads of all the tokens, four loads ahead.
+// them - and goes through all heads of all the tokens, one after the other: what is read may be what the store before it wrote (in place), so the compiler
+// keeps a head's loads behind the stores of the one before.  What is in flight is many waves' (seven or eight to a SIMD), not many loads of one.
 // An angle is position * inv_freq: a product of 31 and 24 bits, formed in 64, as turns, of which only the fraction is kept; cosine and sine
 // of that are fp32.
 // Measured: 20240 tokens of 40 heads (bf16, 128 channels; 414 MB read and written) 68.4 us, 6.1 TB/s, where a large copy reaches 4.9.

@@ -16,9 +16,10 @@
 // the reads of K (16 bytes of eight rows at once) nor the transposed reads of V (32 bytes of four rows) meet in a bank.
 // Masks: a tile that all rows of a wave see whole costs nothing, others are masked element by element, tiles that no row sees are left out.
 // Measured, 32 query heads in groups of four of 128 channels, bf16, results in bf16: 8192 tokens of documents over a cache of 16384 919-985 us, 1.0 PFLOP/s
-// of what the masks leave; 16384 causal tokens 1938-2060 us, 1.07-1.13; 4096 causal tokens 161-170 us, 0.83: two tiles to a place, of which the last to end
+// of what the masks leave; 16384 causal tokens 1938-2060 us, 1.07-1.13; 4096 causal tokens 148-170 us, 0.81-0.93: two tiles to a place, of which the last to end
 // leave their neighbours' places empty for 30 us, and 3 us to begin a tile, 3 to end it.  A library product of 8192^3
-// reaches 1.12.  Of the first (966 when it was taken apart) the loads are 118, the exponentials and maxima 104, LDS reads 24; matrix instructions and
+// reaches 1.12.  With results in fp32 (P in three terms) the first takes 1564-1650, 4096 causal tokens 240-255.
+// Of the first in bf16 (966 when it was taken apart) the loads are 118, the exponentials and maxima 104, LDS reads 24; matrix instructions and
 // barriers alone need 673.  Tried: the next tile's scores between this tile's weights, 962-988; one V buffer and three waves per SIMD, spills, 1134.
 // fp32: 252 tokens of six users over 4474 earlier ones, 64 heads in groups of eight, 2033 us, 112 TFLOP/s, with a cap 2260; 2048 causal tokens, groups of
 // four, 375 us, 92 (a library product: 154; the matrix units are busy 71 % of a busy unit's time, and tiles of 128 rows compute what the diagonal masks).

@@ -249,7 +249,9 @@ struct TokTables {
     int64_t n_items() const { return (int64_t)(items[0].size() + items[1].size() + items[2].size()); }
 };
 
-// Workgroups that run side by side on a compute unit: three of the few kernel's 16-row form (at most 168 registers), two of the others.
+// Workgroups that run side by side on a compute unit, as the rule below counts them: three of the few kernel's 16-row form, two of the others.  That is what fits
+// with 128 channels (149-158 registers; 179-246).  With 64 channels more may fit (16 rows three to five, 93-134 registers; 32 rows three or four; many rows two or
+// three, 145-170), but counting three there made calls no faster, or 5 % slower.
 inline int resident(TokKernel k) { return k == TokKernel::kFew16 ? 3 : 2; }
 
 struct TokTile {

@@ -140,7 +140,7 @@ class TokenStep:
 
     `view` is the cache that takes the tokens: its lengths already count them, n_new[u] of user u.  With `prompt` (the other owner's view of
     the same users) the sequence begins there: the tokens attend to both caches, and the two partials are merged as in Theorem 1.  `rope`, and the
-    keywords of Score that concern a sequence (cap, slopes, causal, window, prefix, ranges), are the model's.  Holds the result buffers.  The views'
+    keywords of Score that concern a sequence (cap, slopes, causal, window, prefix, ranges), are the model's.  Holds the result buffers, which are fp32.  The views'
     lengths are read at every run, so a loop may move them on."""
 
     def __init__(self, ctx: Context, dtype, n_q_heads: int, n_kv_heads: int, head_dim: int, scale: float, view: KVView, n_new,
