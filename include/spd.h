@@ -416,7 +416,8 @@ int spd_append_tokens(spd_ctx *ctx, const spd_shape *shape, const spd_kv_view *v
  *   pos_k < prefix[u]   or   (pos_k <= pos_q if causal, and |pos_q - pos_k| < window if window > 0).
  * A query that sees no key has A = 0 and lse = -inf.  What a key holds that a query does not see - infinities and NaN
  * among it - does not reach that query's result.  A value that is not finite makes the results of the queries that see it
- * not finite in its channel (infinite or NaN), and no others.
+ * not finite in its channel (infinite or NaN), and no others.  (Sums over keys are fp32 before they are divided: finite are
+ * values whose magnitude times 2^8 times the keys that a query sees is.)
  */
 typedef struct spd_score {
     float cap;              /* 0 (none) or positive, at most 1e30, scale / cap neither subnormal nor near overflow  */
