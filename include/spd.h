@@ -454,6 +454,84 @@ int spd_partial_attn_tokens(spd_ctx *ctx, const spd_shape *shape, const void *q,
                             const spd_kv_view *view, const int32_t *n_new, const spd_score *score, void *out,
                             int32_t out_dtype, float *lse, void *hip_stream);
 
+/* ------------------------------------------------------------------------------------------------------------
+ * Trees of drafted tokens: several continuations of a user's sequence, checked at once.  The drafted tokens of user u are n_new[u] new
+ * tokens like those above, in any order in which a token comes behind its parent; a token's branch is the token itself, its parent, that one's
+ * parent and so on.  One step: spd_tree_plan, then in every layer spd_append_tokens (positions from the plan) and spd_partial_attn_tree; and
+ * when it is known which tokens are accepted, spd_keep_tokens for all layers, and shorter lengths.
+ */
+#define SPD_MAX_TREE_WORDS 16
+typedef struct spd_tree {
+    int32_t n_words;       /* 64-bit words of a token's set: 1 .. SPD_MAX_TREE_WORDS; no user has more than 64 * n_words tokens           */
+    const uint64_t *seen;  /* DEVICE [T][n_words]: bit j % 64 of word j / 64: the token sees its user's new token j.  Bits behind the user's
+                              last token mean nothing                                                                                      */
+    const int32_t *depth;  /* DEVICE [T] how many parents a token has; taken as 0 .. n_new[u] - 1, the nearest                              */
+} spd_tree;
+
+/*
+ * From every token's parent its branch and its depth, and, with first and positions (both or neither), its position.
+ *   n_new      HOST [n_users], 0 .. 64 * n_words
+ *   parents    DEVICE int32 [T], a token's number among its user's (0: the first).  What is not an earlier token's number (-1, say) stands for
+ *              none: the token follows what the cache holds.
+ *   first      HOST [n_users], 0 .. 2^30: the position of tokens of depth 0
+ *   seen, depth  as in spd_tree: the set is the branch; all n_words words are written
+ *   positions  DEVICE int32 [T]: first[u] + depth, for spd_append_tokens
+ * Sets and depths do not depend on a layer: one call serves them all.  Launches kernels and nothing else: it may always be recorded.
+ */
+int spd_tree_plan(spd_ctx *ctx, int32_t n_users, const int32_t *n_new, const int32_t *parents, const int32_t *first, int32_t n_words,
+                  uint64_t *seen, int32_t *depth, int32_t *positions, void *hip_stream);
+
+/*
+ * spd_partial_attn_tokens where a user's new tokens are a tree's.  Without score->q_pos they are the view's last n_new[u] tokens: a query sees of
+ * them those in its set (itself among them only if its own bit is set), and of the keys in front of them what the score's masks leave.  With
+ * q_pos the view holds none of them (another owner's cache) and the sets say nothing.  Positions: user u's token t has q_pos[u] + depth[t],
+ * or, without q_pos, k_pos[u] + lens[u] - n_new[u] + depth[t], as a query and as a key; distances, windows and ranges go by these.  The score's prefix
+ * is one of the keys in front of the tree; causal makes no difference among the tree's own keys.
+ * Everything else is as there: results, their roundings, recording and scratch memory (it is the same entry point's).
+ */
+int spd_partial_attn_tree(spd_ctx *ctx, const spd_shape *shape, const void *q, int64_t q_token_stride, const spd_kv_view *view,
+                          const int32_t *n_new, const spd_tree *tree, const spd_score *score, void *out, int32_t out_dtype, float *lse,
+                          void *hip_stream);
+
+/*
+ * Moves tokens of caches together, in place: with b = lens[u] - n_last[u], the place b + i of user u gets what the place
+ * b + keep[t0 + i] held before the call, for i < n_keep[u] (t0: the sum of the n_last in front of u's), in K and V, in all heads of
+ * all the views.  After a check: n_last = the drafted tokens, keep = the accepted branch.  For a cache that is to hold less: n_last =
+ * lens, keep = the tokens that stay.  The caller's lengths are its own to shorten.
+ *   views    HOST [n_views], 0 .. 1024: the layers' caches, with the same lengths, strides and kind of storage; no cache twice
+ *   n_last   HOST [n_users], 0 .. lens[u]; T = their sum, T * Hq at most 2^31 - 1
+ *   keep     DEVICE int32 [T], of user u's n_last[u] entries the first n_keep[u]: any with i <= keep[t0 + i] < n_last[u], in any order, the
+ *            same one more than once if need be.  An entry that is not in that range leaves its place as it is.
+ *   n_keep   DEVICE int32 [n_users]; taken as 0 .. n_last[u], the nearest
+ * No two users may share a page in which places change or are read.  Buffers given by host pointers alone: run the call once eagerly before
+ * it is recorded (it uploads a table of the pointers and remembers it).
+ */
+int spd_keep_tokens(spd_ctx *ctx, const spd_shape *shape, const spd_kv_view *views, int32_t n_views, const int32_t *n_last, const int32_t *keep,
+                    const int32_t *n_keep, void *hip_stream);
+
+/*
+ * Copies pages within the pools of K and of V, in all the views: for a user that forks (a copy of the page in which both go on writing; the
+ * pages before it can be shared through the block tables), and to move or compact what a pool holds.
+ *   views    HOST [n_views], 0 .. 1024: paged, with the same page size and strides; only the pools and these are looked at
+ *   n_pages  pages of every pool
+ *   pairs    DEVICE int32 [n_pairs][2]: from page, to page.  A page that is copied to may be in no other pair, or its contents are undefined;
+ *            pairs with a number outside 0 .. n_pages - 1, or twice the same one, are left out.
+ *   n_tokens DEVICE int32 [n_pairs]: only so many first tokens of the page, the nearest of 0 .. block_size; NULL: all of them
+ * Launches kernels and nothing else: it may always be recorded.
+ */
+int spd_copy_pages(spd_ctx *ctx, const spd_shape *shape, const spd_kv_view *views, int32_t n_views, int32_t n_pages, int32_t n_pairs,
+                   const int32_t *pairs, const int32_t *n_tokens, void *hip_stream);
+
+/* The validation that the four calls perform first (host only, no GPU needed). */
+int spd_validate_tree_plan(int32_t n_users, const int32_t *n_new, const int32_t *parents, const int32_t *first, int32_t n_words,
+                           const uint64_t *seen, const int32_t *depth, const int32_t *positions);
+int spd_validate_tree(const spd_shape *shape, const void *q, int64_t q_token_stride, const spd_kv_view *view, const int32_t *n_new,
+                      const spd_tree *tree, const spd_score *score, const void *out, int32_t out_dtype, const float *lse);
+int spd_validate_keep(const spd_shape *shape, const spd_kv_view *views, int32_t n_views, const int32_t *n_last, const int32_t *keep,
+                      const int32_t *n_keep);
+int spd_validate_pages(const spd_shape *shape, const spd_kv_view *views, int32_t n_views, int32_t n_pages, int32_t n_pairs, const int32_t *pairs,
+                       const int32_t *n_tokens);
+
 /* The validation that spd_partial_attn_tokens and spd_append_tokens perform first (host only, no GPU needed). */
 int spd_validate_tokens(const spd_shape *shape, const void *q, int64_t q_token_stride, const spd_kv_view *view,
                         const int32_t *n_new, const spd_score *score, const void *out, int32_t out_dtype,

@@ -31,6 +31,8 @@ EXPORTED_SYMBOLS = (
     "spd_abi_version", "spd_decode_step_static", "spd_set_option", "spd_get_option",
     "spd_get_last_kernel_instance", "spd_rotate", "spd_append_tokens", "spd_partial_attn_tokens",
     "spd_validate_rotate", "spd_validate_append", "spd_validate_tokens",
+    "spd_tree_plan", "spd_partial_attn_tree", "spd_keep_tokens", "spd_copy_pages",
+    "spd_validate_tree_plan", "spd_validate_tree", "spd_validate_keep", "spd_validate_pages",
 )
 
 SPD_ABI_VERSION = 4      # include/spd.h's; checked against the loaded library below
@@ -67,6 +69,10 @@ class spd_rope(C.Structure):
 class spd_score(C.Structure):
     _fields_ = [("cap", C.c_float), ("slopes", C.c_void_p), ("causal", C.c_int32), ("window", C.c_int32),
                 ("prefix", C.c_void_p), ("ranges", C.c_void_p), ("q_pos", C.c_void_p), ("k_pos", C.c_void_p)]
+
+
+class spd_tree(C.Structure):
+    _fields_ = [("n_words", C.c_int32), ("seen", C.c_void_p), ("depth", C.c_void_p)]
 
 
 class spd_work_item(C.Structure):
@@ -144,8 +150,21 @@ def _load() -> C.CDLL:
     tokens = [shape, vp, i64, view, vp, score, vp, i32, fp]
     lib.spd_partial_attn_tokens.argtypes = [vp, *tokens, vp]
     lib.spd_validate_tokens.argtypes = tokens
+    plan = [i32, vp, vp, vp, i32, vp, vp, vp]
+    lib.spd_tree_plan.argtypes = [vp, *plan, vp]
+    lib.spd_validate_tree_plan.argtypes = plan
+    tree = [shape, vp, i64, view, vp, C.POINTER(spd_tree), score, vp, i32, fp]
+    lib.spd_partial_attn_tree.argtypes = [vp, *tree, vp]
+    lib.spd_validate_tree.argtypes = tree
+    keep = [shape, view, i32, vp, vp, vp]
+    lib.spd_keep_tokens.argtypes = [vp, *keep, vp]
+    lib.spd_validate_keep.argtypes = keep
+    pages = [shape, view, i32, i32, i32, vp, vp]
+    lib.spd_copy_pages.argtypes = [vp, *pages, vp]
+    lib.spd_validate_pages.argtypes = pages
     for name in ("spd_rotate", "spd_append_tokens", "spd_partial_attn_tokens", "spd_validate_rotate", "spd_validate_append",
-                 "spd_validate_tokens"):
+                 "spd_validate_tokens", "spd_tree_plan", "spd_partial_attn_tree", "spd_keep_tokens", "spd_copy_pages", "spd_validate_tree_plan",
+                 "spd_validate_tree", "spd_validate_keep", "spd_validate_pages"):
         getattr(lib, name).restype = C.c_int
     return lib
 
@@ -161,6 +180,11 @@ def make_shape(dtype, n_q_heads: int, n_kv_heads: int, head_dim: int, scale: flo
     if isinstance(dtype, torch.dtype):
         dtype = {torch.float32: SPD_F32, torch.bfloat16: SPD_BF16, torch.float16: SPD_F16}[dtype]
     return spd_shape(int(dtype), int(n_q_heads), int(n_kv_heads), int(head_dim), float(scale))
+
+
+def _pool_pages(pool: torch.Tensor, block_stride: int) -> int:
+    """Pages of a pool: its first dimension, where that counts pages, else as many as lie in it end to end."""
+    return int(pool.shape[0]) if pool.dim() > 1 and pool.stride(0) == block_stride else pool.numel() // max(1, block_stride)
 
 
 class KVView:
@@ -199,8 +223,10 @@ class KVView:
                 st.k_ptrs_dev, st.v_ptrs_dev = self._kp_dev.data_ptr(), self._vp_dev.data_ptr()
         else:
             st.k_pool, st.v_pool = k_pool.data_ptr(), v_pool.data_ptr()
-            st.block_table = block_table.data_ptr()
-            st.max_blocks = int(block_table.shape[1] if max_blocks is None else max_blocks)
+            self.n_pages = min(_pool_pages(t, int(block_stride)) for t in (k_pool, v_pool))
+            if block_table is not None:      # (copies of pages go without one)
+                st.block_table = block_table.data_ptr()
+                st.max_blocks = int(block_table.shape[1] if max_blocks is None else max_blocks)
         self.struct = st
 
     @classmethod
@@ -261,6 +287,34 @@ class Score:
             assert a.shape == (n_users,)
         assert self.slopes is None or self.slopes.numel() == n_q_heads
         assert self.ranges is None or self.ranges.shape[0] == n_tokens
+
+
+class Tree:
+    """Marshalled spd_tree: of every drafted token (of all users, one user after the other) which of its user's drafted tokens it sees (seen: int64
+    [T, words], a bit each, read as unsigned) and its depth (int32 [T]); positions (int32 [T], or None) are what spd_tree_plan makes of the
+    depths.  Keeps the tensors alive."""
+
+    def __init__(self, n_tokens: int, words: int = 1, device="cuda:0"):
+        self._set(torch.empty((n_tokens, words), device=device, dtype=torch.int64), torch.empty(n_tokens, device=device, dtype=torch.int32),
+                  torch.empty(n_tokens, device=device, dtype=torch.int32))
+
+    @classmethod
+    def of(cls, seen: torch.Tensor, depth: torch.Tensor, positions: Optional[torch.Tensor] = None) -> "Tree":
+        tree = cls.__new__(cls)
+        tree._set(seen, depth, positions)
+        return tree
+
+    def _set(self, seen, depth, positions):
+        assert seen.dtype is torch.int64 and seen.is_contiguous() and seen.dim() == 2
+        assert depth.dtype is torch.int32 and depth.is_contiguous() and depth.shape == (seen.shape[0],)
+        assert positions is None or (positions.dtype is torch.int32 and positions.is_contiguous() and positions.shape == depth.shape)
+        self.seen, self.depth, self.positions = seen, depth, positions
+        self.struct = spd_tree(int(seen.shape[1]), seen.data_ptr(), depth.data_ptr())
+
+
+def _view_array(views):
+    """The structs of several views, side by side."""
+    return (spd_kv_view * max(1, len(views)))(*[v.struct for v in views])
 
 
 def _new_counts(n_new, n_users: int):
@@ -555,10 +609,7 @@ class Context:
         self._check(rc, "spd_append_tokens")
         return q_out if q is not None else None
 
-    def spd_partial_attn_tokens(self, shape, q, view: KVView, n_new, score: Optional[Score] = None, out=None, lse=None, out_dtype=None,
-                                stream=None):
-        """Partial attention of every user's n_new[u] tokens (q: [T][Hq][d]) over its keys in the view.  out: [T][Hq][d] in fp32 or the
-        inputs' type (out_dtype where out is not given; default fp32).  Returns (out, lse)."""
+    def _attend_tokens(self, name, shape, q, view: KVView, n_new, tree: Optional[Tree], score: Optional[Score], out, lse, out_dtype, stream):
         counts, T = _new_counts(n_new, view.struct.n_users)
         Hq, d, dtype = shape.n_q_heads, shape.head_dim, _CODE_DTYPES[shape.dtype]
         if out is None:
@@ -572,11 +623,81 @@ class Context:
         if score is not None:
             score.check(view.struct.n_users, T, Hq)
             self._here(None, score.slopes, score.ranges)
-        rc = lib.spd_partial_attn_tokens(self.handle, C.byref(shape), q.data_ptr(), qs, C.byref(view.struct), _address(counts),
-                                         None if score is None else C.byref(score.struct), out.data_ptr(), _DTYPE_CODES[out.dtype],
-                                         lse.data_ptr(), _stream_ptr(stream, self.device))
-        self._check(rc, "spd_partial_attn_tokens")
+        rest = (None if score is None else C.byref(score.struct), out.data_ptr(), _DTYPE_CODES[out.dtype], lse.data_ptr(),
+                _stream_ptr(stream, self.device))
+        first = (self.handle, C.byref(shape), q.data_ptr(), qs, C.byref(view.struct), _address(counts))
+        if tree is None:
+            rc = lib.spd_partial_attn_tokens(*first, *rest)
+        else:
+            assert tree.seen.shape[0] == T
+            self._here(None, tree.seen, tree.depth)
+            rc = lib.spd_partial_attn_tree(*first, C.byref(tree.struct), *rest)
+        self._check(rc, name)
         return out, lse
+
+    def spd_partial_attn_tokens(self, shape, q, view: KVView, n_new, score: Optional[Score] = None, out=None, lse=None, out_dtype=None,
+                                stream=None):
+        """Partial attention of every user's n_new[u] tokens (q: [T][Hq][d]) over its keys in the view.  out: [T][Hq][d] in fp32 or the
+        inputs' type (out_dtype where out is not given; default fp32).  Returns (out, lse)."""
+        return self._attend_tokens("spd_partial_attn_tokens", shape, q, view, n_new, None, score, out, lse, out_dtype, stream)
+
+    def spd_tree_plan(self, parents: torch.Tensor, n_new, first=None, words: Optional[int] = None, tree: Optional[Tree] = None, stream=None) -> Tree:
+        """The Tree of drafted tokens from their parents (int32 [T]: a number among the user's own drafted tokens, -1: none), n_new[u] of user u;
+        with first (a host sequence: the position of each user's tokens without a parent) its positions too.  tree: one to write into."""
+        counts = np.ascontiguousarray(n_new, dtype=np.int32)
+        assert counts.ndim == 1
+        counts, T = _new_counts(counts, counts.shape[0])
+        if tree is None:
+            tree = Tree(T, max(1, -(-int(counts.max(initial=0)) // 64)) if words is None else words, device=parents.device)
+        assert words is None or tree.struct.n_words == words
+        assert parents.dtype is torch.int32 and parents.is_contiguous() and parents.shape == (T,) and tree.seen.shape[0] == T
+        begin = None
+        if first is not None:
+            begin = np.ascontiguousarray(first, dtype=np.int32)
+            assert begin.shape == counts.shape and tree.positions is not None
+        self._here(None, parents, tree.seen, tree.depth, tree.positions if first is not None else None)
+        rc = lib.spd_tree_plan(self.handle, counts.shape[0], _address(counts), parents.data_ptr(), None if begin is None else _address(begin),
+                               tree.struct.n_words, tree.seen.data_ptr(), tree.depth.data_ptr(), None if begin is None else tree.positions.data_ptr(),
+                               _stream_ptr(stream, self.device))
+        self._check(rc, "spd_tree_plan")
+        return tree
+
+    def spd_partial_attn_tree(self, shape, q, view: KVView, n_new, tree: Tree, score: Optional[Score] = None, out=None, lse=None, out_dtype=None,
+                              stream=None):
+        """spd_partial_attn_tokens where every user's new tokens are a tree's: among themselves they see what their sets say, and their positions
+        go by their depths.  Without the score's q_pos they are the view's last tokens."""
+        assert tree is not None
+        return self._attend_tokens("spd_partial_attn_tree", shape, q, view, n_new, tree, score, out, lse, out_dtype, stream)
+
+    def spd_keep_tokens(self, shape, views: Sequence[KVView], n_last, keep: torch.Tensor, n_keep: torch.Tensor, stream=None):
+        """In all the views (the layers' caches), of every user's last n_last[u] tokens those that its part of keep names (int32 [T], of n_last[u]
+        entries the first n_keep[u]) move together, in place: place i gets what lay at keep[i] >= i.  The views' lengths stay as they are."""
+        if not views:
+            return
+        counts, T = _new_counts(n_last, views[0].struct.n_users)
+        for t, n in ((keep, T), (n_keep, counts.shape[0])):
+            assert t.dtype is torch.int32 and t.is_contiguous() and t.shape == (n,)
+        for v in views:
+            self._here(v)
+        self._here(None, keep, n_keep)
+        rc = lib.spd_keep_tokens(self.handle, C.byref(shape), _view_array(views), len(views), _address(counts), keep.data_ptr(), n_keep.data_ptr(),
+                                 _stream_ptr(stream, self.device))
+        self._check(rc, "spd_keep_tokens")
+
+    def spd_copy_pages(self, shape, views: Sequence[KVView], pairs: torch.Tensor, n_tokens: Optional[torch.Tensor] = None, stream=None):
+        """In all the (paged) views' pools, pages copied: pairs int32 [n, 2], from page and to page; n_tokens (int32 [n]): only so many first tokens
+        of each.  A page that is copied to may be in no other pair."""
+        if not views:
+            return
+        assert pairs.dtype is torch.int32 and pairs.is_contiguous() and pairs.dim() == 2 and pairs.shape[1] == 2
+        assert n_tokens is None or (n_tokens.dtype is torch.int32 and n_tokens.is_contiguous() and n_tokens.shape == (pairs.shape[0],))
+        for v in views:
+            assert v.struct.block_size
+            self._here(v)
+        self._here(None, pairs, n_tokens)
+        rc = lib.spd_copy_pages(self.handle, C.byref(shape), _view_array(views), len(views), min(v.n_pages for v in views), pairs.shape[0],
+                                pairs.data_ptr(), None if n_tokens is None else n_tokens.data_ptr(), _stream_ptr(stream, self.device))
+        self._check(rc, "spd_copy_pages")
 
 
 def spd_validate_partial(shape: spd_shape, q_ptr, view: spd_kv_view, out_ptr, lse_ptr) -> int:

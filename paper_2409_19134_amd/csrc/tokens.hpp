@@ -45,6 +45,14 @@ struct ScoreArgs {
     int32_t causal, window;
 };
 
+// A user's new tokens as a tree: which of them each sees, and how deep it lies (its position is the first's and its depth).
+struct TreeArgs {
+    const uint64_t *seen;   // [T][words], a bit for every one of the user's new tokens
+    const int32_t *depth;   // [T]
+    int32_t words;
+    int32_t inside;         // 1: they are the view's last keys; 0: the view holds none of them
+};
+
 struct TokArgs {
     const TokItem *items;
     const TokUser *users;
@@ -64,6 +72,7 @@ struct TokArgs {
     float *part_o;    // [slot][rows of a tile][D]
     float2 *part_lse; // [slot][rows of a tile]: log2 of the sum, and what the final lse adds to it (natural log)
     ScoreArgs score;
+    TreeArgs tree;    // the kernels' tree form
 };
 
 // A query row's masks and bias (slope: its head's, 0 without).  It sees the keys in [mlo, mlo + mn) and in [plo, plo + pn).
@@ -221,6 +230,75 @@ struct KeyWalk {
     __host__ __device__ __forceinline__ int next(int t) const { return over_gap(t + round); }  // t < hi
 };
 
+// Trees.  Depths are what the caller's memory holds: they are kept to what a tree of so many tokens can have.
+__device__ __forceinline__ int tree_depth(const TokArgs &a, const TokUser &u, int token) { return clampi(a.tree.depth[u.tok0 + token], 0, u.n_tok - 1); }
+// The view's keys in front of the tree: those that order, windows, prefixes and ranges decide about.
+template <bool TREE>
+__device__ __forceinline__ int plain_keys(const TokArgs &a, const TokUser &u, int len)
+{
+    return TREE && a.tree.inside ? len - u.n_tok : len;
+}
+// A token's masks.  (Inside the view, a tree's token is its own nearest key.)
+template <bool TREE>
+__device__ __forceinline__ RowMask token_mask(const TokArgs &a, const TokUser &u, int len, int q_pos0, int token, float slope)
+{
+    RowMask r = row_mask(a.score, u, plain_keys<TREE>(a, u, len), q_pos0 + (TREE ? tree_depth(a, u, token) : token), token, slope);
+    if (TREE && a.tree.inside)
+        r.dist0 = 0;
+    return r;
+}
+// ... of a tile's rows `first` .. `last` without ranges.  A tree's tokens lie at any depth, in any order.
+template <bool TREE>
+__device__ __forceinline__ Limits token_limits(const TokArgs &a, const TokUser &u, int len, int q_pos0, int first, int last)
+{
+    return tile_limits(a.score, u, plain_keys<TREE>(a, u, len), q_pos0 + (TREE ? 0 : first), q_pos0 + (TREE ? u.n_tok - 1 : last));
+}
+// The tree's own keys, which some row sees and not every one.
+template <bool TREE>
+__device__ __forceinline__ void add_tree(Limits &l, const TokArgs &a, const TokUser &u, int len)
+{
+    if (TREE && a.tree.inside) {
+        const int base = len - u.n_tok;
+        l.any_lo = min(l.any_lo, base);
+        l.win_lo = min(l.win_lo, base);
+        l.any_hi = len;
+        l.full_hi = min(l.full_hi, base);
+    }
+}
+// Which of the `n` (up to 64) keys from `key` on a tree's token sees as tokens of the tree, which begins at key `base`.
+__device__ __forceinline__ uint64_t tree_sees(const TokArgs &a, const TokUser &u, int base, int token, int q_pos, int key, int n)
+{
+    const int first = key - base, word = first >> 6, shift = first & 63;
+    const uint64_t *const set = a.tree.seen + (int64_t)(u.tok0 + token) * a.tree.words;
+    uint64_t bits = 0;
+    if ((unsigned)word < (unsigned)a.tree.words)
+        bits = set[word] >> shift;
+    if (shift && (unsigned)(word + 1) < (unsigned)a.tree.words)
+        bits |= set[word + 1] << (64 - shift);
+    const int left = min(n, u.n_tok - first);  // (bits behind the last token mean nothing)
+    bits &= left >= 64 ? ~0ull : left > 0 ? (1ull << left) - 1 : 0ull;
+    // windows shorter than the tree may be deep, and documents
+    if (a.score.ranges || (a.score.window && a.score.window < u.n_tok)) {
+        int lo = 0, hi = 0x7fffffff;
+        if (a.score.ranges) {
+            const int2 v = reinterpret_cast<const int2 *>(a.score.ranges)[u.tok0 + token];
+            lo = max(v.x, 0) - u.k_pos;
+            hi = max(v.y, 0) - u.k_pos;
+        }
+        for (uint64_t rest = bits; rest; rest &= rest - 1) {
+            const int pos = base + tree_depth(a, u, first + __builtin_ctzll(rest));
+            if (pos < lo || pos >= hi || (a.score.window && abs(q_pos - pos) >= a.score.window))
+                bits &= ~(rest & -rest);
+        }
+    }
+    return bits;
+}
+// The distance of a query to a key, which may be one of the tree's.
+__device__ __forceinline__ int tree_apart(const TokArgs &a, const TokUser &u, int base, int q_pos, int key)
+{
+    return q_pos - (key < base ? key : base + tree_depth(a, u, min(key - base, u.n_tok - 1)));
+}
+
 // A row's view of a run of keys from key0 on, made anew for every run: without the detour the compiler keeps every key's differences to the row's
 // limits in registers, over all runs.
 struct RunMask {
@@ -348,10 +426,10 @@ __device__ __forceinline__ void store4(const TokArgs &a, int64_t at, f32x4 v)
 }
 
 // Launches (host): `rows` is the row capacity of the few kernel's tiles, 16 or 32.
-__attribute__((visibility("hidden"))) void launch_tokens_few(int dtype, int head_dim, bool paged, int rows, bool modified, int64_t n_items,
-                                                             const TokArgs &a, hipStream_t stream);
-__attribute__((visibility("hidden"))) void launch_tokens_many(int dtype, int head_dim, bool modified, int64_t n_items, const TokArgs &a,
-                                                              hipStream_t stream);
+__attribute__((visibility("hidden"))) void launch_tokens_few(int dtype, int head_dim, bool paged, int rows, bool modified, bool tree,
+                                                             int64_t n_items, const TokArgs &a, hipStream_t stream);
+__attribute__((visibility("hidden"))) void launch_tokens_many(int dtype, int head_dim, bool modified, bool tree, int64_t n_items,
+                                                              const TokArgs &a, hipStream_t stream);
 constexpr int kManyRows = 128;  // rows of a tile of the many kernel
 __host__ __device__ constexpr int many_keys(int dtype) { return dtype == SPD_F32 ? 32 : 64; }  // keys of its steps
 constexpr int kFewKeys = 32;    // keys that the few kernel's stretches are multiples of

@@ -4,10 +4,12 @@
 
 #include <new>
 
+#include "cache_moves.hpp"
 #include "context.hpp"
 #include "rotary.hpp"
 #include "schedule_key.hpp"
 #include "tokens_schedule.hpp"
+#include "tree_plan.hpp"
 
 namespace spd {
 
@@ -94,8 +96,8 @@ struct TokEntry {
 };
 
 struct TokensState {
-    std::vector<TokEntry> entries[2];  // attention, append
-    char *slab_dev[2] = {nullptr, nullptr}, *slab_pinned[2] = {nullptr, nullptr};
+    std::vector<TokEntry> entries[3];  // attention, append, moves within caches
+    char *slab_dev[3] = {}, *slab_pinned[3] = {};
     uint64_t tick = 0;
     size_t latest = 0;          // the attention's entry that the latest call used
     float *part = nullptr;      // scratch memory of the attention: [slots][rows][D], then float2 [slots][rows]
@@ -170,7 +172,7 @@ void free_state(TokensState *t)
             if (e.uploaded)
                 (void)hipEventDestroy(e.uploaded);
         }
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < 3; ++i) {
         if (t->slab_dev[i])
             (void)hipFree(t->slab_dev[i]);
         if (t->slab_pinned[i])
@@ -349,15 +351,15 @@ int32_t growth(const std::vector<int32_t> &was, const std::vector<int32_t> &now)
 
 size_t padded(size_t n) { return (n + 255) / 256 * 256; }
 
-int find_or_build(ContextBase *ctx, TokensState *t, const spd_shape *s, const spd_kv_view *v, const spd_score *c, hipStream_t stream, bool in_graph,
-                  TokEntry **out, int32_t *grow_len, int32_t *grow_q)
+int find_or_build(ContextBase *ctx, TokensState *t, const spd_shape *s, const spd_kv_view *v, const spd_score *c, bool tree, hipStream_t stream,
+                  bool in_graph, TokEntry **out, int32_t *grow_len, int32_t *grow_q)
 {
     const int causal = c ? c->causal : 0, window = c ? c->window : 0;
     t->lens.clear();
     t->q_pos.clear();
     KeyWriter w(t->key, 64 + (size_t)v->n_users * (12 + kStorageBytes));
     const int32_t head[9] = {s->dtype, s->n_q_heads, s->n_kv_heads, s->head_dim, v->n_users, v->block_size, causal, window,
-                             (v->block_size == 0 && v->k_ptrs_dev) ? 1 : 0};
+                             ((v->block_size == 0 && v->k_ptrs_dev) ? 1 : 0) | (tree ? 2 : 0)};
     w.put(head);
     w.put(v->head_stride);
     for (int u = 0; u < v->n_users; ++u) {
@@ -403,7 +405,7 @@ int find_or_build(ContextBase *ctx, TokensState *t, const spd_shape *s, const sp
     if (in_graph)
         return cannot_record(ctx);
     TokTables T;
-    build_tok_tables(s, v, t->plan, causal, window, ctx->n_cus, T);
+    build_tok_tables(s, v, t->plan, causal, window, ctx->n_cus, T, tree);
     size_t bytes = padded(T.users.size() * sizeof(TokUser)), off_items[kTokKernels], off_joins[kTokKernels];
     for (int k = 0; k < kTokKernels; ++k) {
         off_items[k] = bytes;
@@ -491,9 +493,9 @@ void launch_join(int head_dim, int64_t n, int max_rows, int max_chunks, const To
 }
 
 int attend(ContextBase *ctx, const spd_shape *s, const void *q, int64_t q_stride, const spd_kv_view *v, const int32_t *n_new, const spd_score *c,
-           void *out, int32_t out_dtype, float *lse, hipStream_t stream)
+           void *out, int32_t out_dtype, float *lse, const spd_tree *tree, hipStream_t stream)
 {
-    int rc = validate_tokens(s, q, q_stride, v, n_new, c, out, out_dtype, lse);
+    int rc = validate_tokens(s, q, q_stride, v, n_new, c, out, out_dtype, lse, tree);
     if (rc != SPD_OK)
         return rc;
     int64_t total = 0;
@@ -508,7 +510,7 @@ int attend(ContextBase *ctx, const spd_shape *s, const void *q, int64_t q_stride
     const bool in_graph = recording(stream);
     TokEntry *e = nullptr;
     int32_t grow_len = 0, grow_q = 0;
-    rc = find_or_build(ctx, t, s, v, c, stream, in_graph, &e, &grow_len, &grow_q);
+    rc = find_or_build(ctx, t, s, v, c, tree != nullptr, stream, in_graph, &e, &grow_len, &grow_q);
     if (rc != SPD_OK)
         return rc;
     size_t rows[kTokKernels], part_rows = 0;
@@ -558,6 +560,12 @@ int attend(ContextBase *ctx, const spd_shape *s, const void *q, int64_t q_stride
         sc.causal = c->causal;
         sc.window = c->window;
     }
+    if (tree) {
+        a.tree.seen = tree->seen;
+        a.tree.depth = tree->depth;
+        a.tree.words = tree->n_words;
+        a.tree.inside = !(c && c->q_pos);
+    }
     const bool modified = sc.cap_out != 0.f || sc.slopes;
     float2 *const part_lse = reinterpret_cast<float2 *>(t->part + part_rows * (size_t)s->head_dim);
     for (int k = 0; k < kTokKernels; ++k) {
@@ -570,9 +578,9 @@ int attend(ContextBase *ctx, const spd_shape *s, const void *q, int64_t q_stride
         in_parts(e->n_items[k], [&](int64_t first, unsigned n) {
             a.items = items + first;
             if (k == (int)TokKernel::kMany)
-                launch_tokens_many(s->dtype, s->head_dim, modified, n, a, stream);
+                launch_tokens_many(s->dtype, s->head_dim, modified, tree != nullptr, n, a, stream);
             else
-                launch_tokens_few(s->dtype, s->head_dim, paged, cap, modified, n, a, stream);
+                launch_tokens_few(s->dtype, s->head_dim, paged, cap, modified, tree != nullptr, n, a, stream);
         });
         SPD_TRY(ctx, hipGetLastError());
         if (e->n_joins[k] == 0)
@@ -767,6 +775,226 @@ int append(ContextBase *ctx, const spd_shape *s, const spd_kv_view *v, const int
     return SPD_OK;
 }
 
+int tree_plan(ContextBase *ctx, int32_t n_users, const int32_t *n_new, const int32_t *parents, const int32_t *first, int32_t words, uint64_t *seen,
+              int32_t *depth, int32_t *positions, hipStream_t stream)
+{
+    const int rc = validate_tree_plan(n_users, n_new, parents, first, words, seen, depth, positions);
+    if (rc != SPD_OK)
+        return rc;
+    PlanArgs a = {};
+    a.parents = parents;
+    a.seen = seen;
+    a.depth = depth;
+    a.positions = positions;
+    a.words = words;
+    const OnDevice on(ctx->device);
+    SPD_TRY(ctx, on.error);
+    // A launch's users travel with its arguments: those that have tokens, so many at a time.
+    PlanUsers users;
+    int32_t token = 0, n = 0, most = 0;
+    auto launch = [&]() -> int {
+        if (n == 0)
+            return SPD_OK;
+        if (most <= 64)
+            hipLaunchKernelGGL(plan_small_kernel, dim3((unsigned)n), dim3(64), 0, stream, a, users);
+        else
+            hipLaunchKernelGGL(plan_kernel, dim3((unsigned)n), dim3(kPlanThreads), 0, stream, a, users);
+        n = most = 0;
+        SPD_TRY(ctx, hipGetLastError());
+        return SPD_OK;
+    };
+    for (int u = 0; u < n_users; ++u) {
+        if (n_new[u] == 0)
+            continue;
+        users.it[n++] = PlanUser{token, n_new[u], first ? first[u] : 0};
+        token += n_new[u];
+        most = std::max(most, n_new[u]);
+        if (n == kPlanUsers) {
+            const int failed = launch();
+            if (failed != SPD_OK)
+                return failed;
+        }
+    }
+    return launch();
+}
+
+// Kernel template arguments from run-time values: bytes of a row, paged.
+template <class F>
+void with_row_bytes(int bytes, F &&f)
+{
+    if (bytes == 128)
+        f(std::integral_constant<int, 128>());
+    else if (bytes == 256)
+        f(std::integral_constant<int, 256>());
+    else
+        f(std::integral_constant<int, 512>());
+}
+
+int keep_tokens(ContextBase *ctx, const spd_shape *s, const spd_kv_view *views, int32_t n_views, const int32_t *n_last, const int32_t *keep,
+                const int32_t *n_keep, hipStream_t stream)
+{
+    int rc = validate_keep(s, views, n_views, n_last, keep, n_keep);
+    if (rc != SPD_OK || n_views == 0)
+        return rc;
+    const spd_kv_view &v = views[0];
+    int64_t total = 0;
+    for (int u = 0; u < v.n_users; ++u)
+        total += n_last[u];
+    if (total == 0)
+        return SPD_OK;
+    const OnDevice on(ctx->device);
+    SPD_TRY(ctx, on.error);
+    const int es = elt_size(s->dtype), U = v.n_users;
+    const bool paged = v.block_size != 0;
+    // Buffers without pointer arrays on the device: the pointers of all layers, remembered by themselves ([layer][K, V][user]).
+    const char *uploaded = nullptr;
+    if (!paged && !v.k_ptrs_dev) {
+        TokensState *t = state_of(ctx);
+        const bool in_graph = recording(stream);
+        const size_t n = (size_t)n_views * 2 * (size_t)U;
+        KeyWriter w(t->key, 16 + n * sizeof(void *));
+        const int32_t head[2] = {n_views, U};
+        w.put(head);
+        for (int i = 0; i < n_views; ++i)
+            for (const void *const *ptrs : {views[i].k_ptrs, views[i].v_ptrs})
+                for (int u = 0; u < U; ++u)
+                    w.put(n_last[u] > 0 ? ptrs[u] : nullptr);
+        w.done();
+        const uint64_t hash = hash_key(t->key.data(), t->key.size());
+        TokEntry *e = find(t->entries[2], t->key, hash);
+        if (e) {
+            use_entry(t, *e, stream, in_graph);
+        } else if (in_graph) {
+            return cannot_record(ctx);
+        } else {
+            const size_t bytes = padded(n * sizeof(void *));
+            rc = new_entry(ctx, t, 2, bytes, stream, &e);
+            if (rc != SPD_OK)
+                return rc;
+            std::memcpy(e->pinned, t->key.data() + sizeof head, n * sizeof(void *));
+            e->key = t->key;
+            e->hash = hash;
+            rc = upload(ctx, t, *e, bytes, stream);
+            if (rc != SPD_OK)
+                return rc;
+        }
+        uploaded = e->dev;
+    }
+    KeepArgs a = {};
+    a.keep = keep;
+    a.n_keep = n_keep;
+    a.token_stride = v.token_stride * es;
+    a.block_stride = paged ? v.block_stride * es : 0;
+    a.max_blocks = paged ? v.max_blocks : 0;
+    a.page_shift = paged ? page_shift(v.block_size) : 0;
+    a.n_heads = s->n_kv_heads;
+    const int row_bytes = s->head_dim * es;
+    KeepUsers users;
+    KeepLayers layers;
+    int failed = SPD_OK;
+    auto launch = [&](int n_users, int n_layers) {
+        const int64_t streams = (int64_t)n_users * n_layers * 2 * s->n_kv_heads;
+        with_row_bytes(row_bytes, [&](auto rb) {
+            // enough waves to fill the device, down to a quarter of the row's cache line to a wave
+            a.slices = 1;
+            while (a.slices * 64 < rb() && streams * a.slices < 8 * (int64_t)ctx->n_cus)
+                a.slices *= 2;
+            in_parts((streams * a.slices + 3) / 4, [&](int64_t first, unsigned n) {
+                a.first = (uint32_t)(first * 4);
+                a.n_waves = (uint32_t)(streams * a.slices);
+                a.n_layers = n_layers;
+                if (paged)
+                    hipLaunchKernelGGL((keep_kernel<rb(), true>), dim3(n), dim3(256), 0, stream, a, users, layers);
+                else
+                    hipLaunchKernelGGL((keep_kernel<rb(), false>), dim3(n), dim3(256), 0, stream, a, users, layers);
+            });
+        });
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) {
+            ctx->last_hip = (int)e;
+            failed = SPD_ERR_HIP;
+        }
+    };
+    int32_t token = 0;
+    for (int u = 0; u < U;) {
+        int n_users = 0;
+        for (; u < U && n_users < kKeepUsers; ++u) {
+            if (n_last[u] == 0)
+                continue;
+            KeepUser &x = users.it[n_users++];
+            x.head_stride = (v.head_strides && !paged ? v.head_strides[u] : v.head_stride) * es;
+            x.user = u;
+            x.token = token;
+            x.begin = v.lens[u] - n_last[u];
+            x.n = n_last[u];
+            token += n_last[u];
+        }
+        for (int i = 0; n_users > 0 && i < n_views && failed == SPD_OK; i += kKeepLayers) {
+            const int n_layers = std::min(n_views - i, kKeepLayers);
+            for (int j = 0; j < n_layers; ++j) {
+                const spd_kv_view &l = views[i + j];
+                KeepLayer &x = layers.it[j];
+                x.table = paged ? l.block_table : nullptr;
+                if (paged) {
+                    x.kv[0] = static_cast<char *>(const_cast<void *>(l.k_pool));
+                    x.kv[1] = static_cast<char *>(const_cast<void *>(l.v_pool));
+                } else if (uploaded) {
+                    for (int kv = 0; kv < 2; ++kv)
+                        x.kv[kv] = const_cast<char *>(uploaded) + ((size_t)(i + j) * 2 + (size_t)kv) * (size_t)U * sizeof(void *);
+                } else {
+                    x.kv[0] = const_cast<char *>(reinterpret_cast<const char *>(l.k_ptrs_dev));
+                    x.kv[1] = const_cast<char *>(reinterpret_cast<const char *>(l.v_ptrs_dev));
+                }
+            }
+            launch(n_users, n_layers);
+        }
+    }
+    return failed;
+}
+
+int copy_pages(ContextBase *ctx, const spd_shape *s, const spd_kv_view *views, int32_t n_views, int32_t n_pages, int32_t n_pairs, const int32_t *pairs,
+               const int32_t *n_tokens, hipStream_t stream)
+{
+    const int rc = validate_pages(s, views, n_views, n_pages, n_pairs, pairs, n_tokens);
+    if (rc != SPD_OK || n_views == 0 || n_pages == 0 || n_pairs == 0)
+        return rc;
+    const OnDevice on(ctx->device);
+    SPD_TRY(ctx, on.error);
+    const spd_kv_view &v = views[0];
+    const int es = elt_size(s->dtype), row_bytes = s->head_dim * es;
+    PageArgs a = {};
+    a.token_stride = v.token_stride * es;
+    a.head_stride = v.head_stride * es;
+    a.block_stride = v.block_stride * es;
+    a.n_pages = n_pages;
+    a.n_heads = s->n_kv_heads;
+    a.page_shift = page_shift(v.block_size);
+    a.token_major = v.head_stride < v.token_stride;
+    a.parts = (int32_t)(((int64_t)s->n_kv_heads * v.block_size * (row_bytes / 16) + kPagePieces - 1) / kPagePieces);
+    PageLayers layers;
+    for (int i = 0; i < n_views; i += kPageLayers) {
+        const int n_layers = std::min(n_views - i, kPageLayers);
+        for (int j = 0; j < n_layers; ++j) {
+            layers.kv[j][0] = static_cast<char *>(const_cast<void *>(views[i + j].k_pool));
+            layers.kv[j][1] = static_cast<char *>(const_cast<void *>(views[i + j].v_pool));
+        }
+        a.n_layers = n_layers;
+        const int64_t groups = (int64_t)n_layers * 2 * a.parts, most = std::max<int64_t>(1, kMostGroups / groups);  // of a pair; pairs of a launch
+        with_row_bytes(row_bytes, [&](auto rb) {
+            for (int64_t p = 0; p < n_pairs; p += most) {
+                a.pairs = pairs + 2 * p;
+                a.n_tokens = n_tokens ? n_tokens + p : nullptr;
+                in_parts(groups * std::min(most, n_pairs - p), [&](int64_t first, unsigned n) {
+                    a.first = (uint32_t)first;
+                    hipLaunchKernelGGL((copy_pages_kernel<rb()>), dim3(n), dim3(256), 0, stream, a, layers);
+                });
+            }
+        });
+        SPD_TRY(ctx, hipGetLastError());
+    }
+    return SPD_OK;
+}
+
 }  // namespace
 }  // namespace spd
 
@@ -844,10 +1072,73 @@ int spd_partial_attn_tokens(spd_ctx *ctx, const spd_shape *shape, const void *q,
 try {
     if (!ctx)
         return SPD_ERR_NULL;
-    return spd::attend(spd::context_base(ctx), shape, q, q_token_stride, view, n_new, score, out, out_dtype, lse,
+    return spd::attend(spd::context_base(ctx), shape, q, q_token_stride, view, n_new, score, out, out_dtype, lse, nullptr,
                        static_cast<hipStream_t>(hip_stream));
 } catch (...) {
     return SPD_ERR_NOMEM;
+}
+
+int spd_validate_tree_plan(int32_t n_users, const int32_t *n_new, const int32_t *parents, const int32_t *first, int32_t n_words,
+                           const uint64_t *seen, const int32_t *depth, const int32_t *positions)
+{
+    return spd::host::validate_tree_plan(n_users, n_new, parents, first, n_words, seen, depth, positions);
+}
+
+int spd_validate_tree(const spd_shape *shape, const void *q, int64_t q_token_stride, const spd_kv_view *view, const int32_t *n_new,
+                      const spd_tree *tree, const spd_score *score, const void *out, int32_t out_dtype, const float *lse)
+{
+    return tree ? spd::host::validate_tokens(shape, q, q_token_stride, view, n_new, score, out, out_dtype, lse, tree) : SPD_ERR_NULL;
+}
+
+int spd_validate_keep(const spd_shape *shape, const spd_kv_view *views, int32_t n_views, const int32_t *n_last, const int32_t *keep,
+                      const int32_t *n_keep)
+{
+    return spd::host::validate_keep(shape, views, n_views, n_last, keep, n_keep);
+}
+
+int spd_validate_pages(const spd_shape *shape, const spd_kv_view *views, int32_t n_views, int32_t n_pages, int32_t n_pairs, const int32_t *pairs,
+                       const int32_t *n_tokens)
+{
+    return spd::host::validate_pages(shape, views, n_views, n_pages, n_pairs, pairs, n_tokens);
+}
+
+int spd_tree_plan(spd_ctx *ctx, int32_t n_users, const int32_t *n_new, const int32_t *parents, const int32_t *first, int32_t n_words,
+                  uint64_t *seen, int32_t *depth, int32_t *positions, void *hip_stream)
+{
+    if (!ctx)
+        return SPD_ERR_NULL;
+    return spd::tree_plan(spd::context_base(ctx), n_users, n_new, parents, first, n_words, seen, depth, positions,
+                          static_cast<hipStream_t>(hip_stream));
+}
+
+int spd_partial_attn_tree(spd_ctx *ctx, const spd_shape *shape, const void *q, int64_t q_token_stride, const spd_kv_view *view,
+                          const int32_t *n_new, const spd_tree *tree, const spd_score *score, void *out, int32_t out_dtype, float *lse,
+                          void *hip_stream)
+try {
+    if (!ctx || !tree)
+        return SPD_ERR_NULL;
+    return spd::attend(spd::context_base(ctx), shape, q, q_token_stride, view, n_new, score, out, out_dtype, lse, tree,
+                       static_cast<hipStream_t>(hip_stream));
+} catch (...) {
+    return SPD_ERR_NOMEM;
+}
+
+int spd_keep_tokens(spd_ctx *ctx, const spd_shape *shape, const spd_kv_view *views, int32_t n_views, const int32_t *n_last, const int32_t *keep,
+                    const int32_t *n_keep, void *hip_stream)
+try {
+    if (!ctx)
+        return SPD_ERR_NULL;
+    return spd::keep_tokens(spd::context_base(ctx), shape, views, n_views, n_last, keep, n_keep, static_cast<hipStream_t>(hip_stream));
+} catch (...) {
+    return SPD_ERR_NOMEM;
+}
+
+int spd_copy_pages(spd_ctx *ctx, const spd_shape *shape, const spd_kv_view *views, int32_t n_views, int32_t n_pages, int32_t n_pairs,
+                   const int32_t *pairs, const int32_t *n_tokens, void *hip_stream)
+{
+    if (!ctx)
+        return SPD_ERR_NULL;
+    return spd::copy_pages(spd::context_base(ctx), shape, views, n_views, n_pages, n_pairs, pairs, n_tokens, static_cast<hipStream_t>(hip_stream));
 }
 
 }  // extern "C"

@@ -93,7 +93,7 @@ __device__ __forceinline__ void keep_finite(VRow<512> &v)
     }
 }
 
-template <int DT, int D, bool PAGED, int NT, bool MOD>
+template <int DT, int D, bool PAGED, int NT, bool MOD, bool TREE>
 __global__ __launch_bounds__(256, 2) void tokens_few_kernel(const TokArgs a)
 {
     constexpr int kBytes = Elt<DT>::kBytes, RB = D * kBytes, NA = step_tiles(RB), NE = 4 * NA, kStep = 16 * NA, CP = D / 16;
@@ -135,14 +135,16 @@ __global__ __launch_bounds__(256, 2) void tokens_few_kernel(const TokArgs a)
     if (a.score.ranges) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
-            lim.add(row_mask(a.score, u, len, q_pos0 + token[nt], token[nt], 0.f));
+            lim.add(token_mask<TREE>(a, u, len, q_pos0, token[nt], 0.f));
 #pragma unroll
         for (int x = 1; x < 16; x *= 2)  // (the four lane groups hold the same rows)
             lim.add(lim.of_lane_xor(x));
         lim = lim.uniform_of();
     } else {
-        lim = tile_limits(a.score, u, len, q_pos0 + it.row0 / a.G, q_pos0 + (it.row0 + it.n_rows - 1) / a.G);
+        lim = token_limits<TREE>(a, u, len, q_pos0, it.row0 / a.G, (it.row0 + it.n_rows - 1) / a.G);
     }
+    add_tree<TREE>(lim, a, u, len);
+    const int tree_begin = TREE ? plain_keys<TREE>(a, u, len) : 0;  // (without the tree inside the view: its end)
     const KeyWalk walk(lim, it.k_begin, k_end, kStep, 4);
     const int hi = walk.hi, full_lo = lim.full_lo, full_hi = min(lim.full_hi, hi);
 
@@ -177,7 +179,7 @@ __global__ __launch_bounds__(256, 2) void tokens_few_kernel(const TokArgs a)
             if (NT > 1 && wave == nt)
                 q_lds[(nt * kQ + kk) * 64 + lane] = qB[kk];
         }
-        mask[nt] = row_mask(a.score, u, len, q_pos0 + token[nt], token[nt], slope[nt]);
+        mask[nt] = token_mask<TREE>(a, u, len, q_pos0, token[nt], slope[nt]);
     }
     if (NT > 1)
         __syncthreads();
@@ -229,12 +231,20 @@ __global__ __launch_bounds__(256, 2) void tokens_few_kernel(const TokArgs a)
             float x[NE];
             const RunMask run(mask[nt], t0);
 #pragma unroll
-            for (int e = 0; e < NE; ++e)
-                x[e] = modified<MOD>(s[e / 4][e % 4], a.score, mask[nt], run.q - e);
-            if (masked)
+            for (int e = 0; e < NE; ++e) {
+                int apart = run.q - e;
+                if (TREE && MOD && a.score.slopes && tb + kStep > tree_begin && a.tree.inside)
+                    apart = tree_apart(a, u, tree_begin, mask[nt].q_pos, t0 + e);
+                x[e] = modified<MOD>(s[e / 4][e % 4], a.score, mask[nt], apart);
+            }
+            if (masked) {
+                uint32_t branch = 0;
+                if (TREE && tb + kStep > tree_begin && a.tree.inside)
+                    branch = (uint32_t)tree_sees(a, u, tree_begin, token[nt], mask[nt].q_pos, t0, NE);
 #pragma unroll
                 for (int e = 0; e < NE; ++e)
-                    x[e] = run.sees(mask[nt], e) ? x[e] : -INFINITY;
+                    x[e] = run.sees(mask[nt], e) || (TREE && (branch >> e & 1u)) ? x[e] : -INFINITY;
+            }
             float mt = x[0];
 #pragma unroll
             for (int e = 1; e < NE; ++e)
@@ -290,7 +300,8 @@ __global__ __launch_bounds__(256, 2) void tokens_few_kernel(const TokArgs a)
                 const char *v = L.v_base + token_offset(a, L.bt_row, key);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    if (!sees(mask[nt], key))
+                    if (!sees(mask[nt], key) &&
+                        !(TREE && a.tree.inside && key >= tree_begin && tree_sees(a, u, tree_begin, token[nt], mask[nt].q_pos, key, 1)))
                         continue;
 #pragma unroll
                     for (int cc = 0; cc < CP; ++cc)
@@ -350,7 +361,7 @@ __global__ __launch_bounds__(256, 2) void tokens_few_kernel(const TokArgs a)
             const int row = it.row0 + nt * 16 + rr, token = row / a.G, head = it.kv_head * a.G + (row - token * a.G);
             float offset = 0.f;
             if (MOD && a.score.slopes && ch == 0) {
-                const RowMask mk = row_mask(a.score, u, len, q_pos0 + token, token, 0.f);
+                const RowMask mk = token_mask<TREE>(a, u, len, q_pos0, token, 0.f);
                 offset = -a.score.slopes[head] * (float)mk.dist0;
             }
             if (it.slot >= 0) {
@@ -367,41 +378,47 @@ __global__ __launch_bounds__(256, 2) void tokens_few_kernel(const TokArgs a)
     }
 }
 
+// Kernel template arguments from run-time values.
 template <int DT, int D, bool PAGED, int NT>
-void launch(bool modified, int64_t n_items, const TokArgs &a, hipStream_t stream)
+void launch(bool modified, bool tree, int64_t n_items, const TokArgs &a, hipStream_t stream)
 {
-    if (modified)
-        hipLaunchKernelGGL((tokens_few_kernel<DT, D, PAGED, NT, true>), dim3((unsigned)n_items), dim3(256), 0, stream, a);
+    const dim3 grid((unsigned)n_items), block(256);
+    if (tree && modified)
+        hipLaunchKernelGGL((tokens_few_kernel<DT, D, PAGED, NT, true, true>), grid, block, 0, stream, a);
+    else if (tree)
+        hipLaunchKernelGGL((tokens_few_kernel<DT, D, PAGED, NT, false, true>), grid, block, 0, stream, a);
+    else if (modified)
+        hipLaunchKernelGGL((tokens_few_kernel<DT, D, PAGED, NT, true, false>), grid, block, 0, stream, a);
     else
-        hipLaunchKernelGGL((tokens_few_kernel<DT, D, PAGED, NT, false>), dim3((unsigned)n_items), dim3(256), 0, stream, a);
+        hipLaunchKernelGGL((tokens_few_kernel<DT, D, PAGED, NT, false, false>), grid, block, 0, stream, a);
 }
 template <int DT, int D>
-void launch(bool paged, int rows, bool modified, int64_t n_items, const TokArgs &a, hipStream_t stream)
+void launch(bool paged, int rows, bool modified, bool tree, int64_t n_items, const TokArgs &a, hipStream_t stream)
 {
     if (rows == 16)
-        paged ? launch<DT, D, true, 1>(modified, n_items, a, stream) : launch<DT, D, false, 1>(modified, n_items, a, stream);
+        paged ? launch<DT, D, true, 1>(modified, tree, n_items, a, stream) : launch<DT, D, false, 1>(modified, tree, n_items, a, stream);
     else
-        paged ? launch<DT, D, true, 2>(modified, n_items, a, stream) : launch<DT, D, false, 2>(modified, n_items, a, stream);
+        paged ? launch<DT, D, true, 2>(modified, tree, n_items, a, stream) : launch<DT, D, false, 2>(modified, tree, n_items, a, stream);
 }
 template <int DT>
-void launch(int head_dim, bool paged, int rows, bool modified, int64_t n_items, const TokArgs &a, hipStream_t stream)
+void launch(int head_dim, bool paged, int rows, bool modified, bool tree, int64_t n_items, const TokArgs &a, hipStream_t stream)
 {
     if (head_dim == 64)
-        launch<DT, 64>(paged, rows, modified, n_items, a, stream);
+        launch<DT, 64>(paged, rows, modified, tree, n_items, a, stream);
     else
-        launch<DT, 128>(paged, rows, modified, n_items, a, stream);
+        launch<DT, 128>(paged, rows, modified, tree, n_items, a, stream);
 }
 
 }  // namespace
 
-void launch_tokens_few(int dtype, int head_dim, bool paged, int rows, bool modified, int64_t n_items, const TokArgs &a, hipStream_t stream)
+void launch_tokens_few(int dtype, int head_dim, bool paged, int rows, bool modified, bool tree, int64_t n_items, const TokArgs &a, hipStream_t stream)
 {
     if (dtype == SPD_F32)
-        launch<SPD_F32>(head_dim, paged, rows, modified, n_items, a, stream);
+        launch<SPD_F32>(head_dim, paged, rows, modified, tree, n_items, a, stream);
     else if (dtype == SPD_BF16)
-        launch<SPD_BF16>(head_dim, paged, rows, modified, n_items, a, stream);
+        launch<SPD_BF16>(head_dim, paged, rows, modified, tree, n_items, a, stream);
     else
-        launch<SPD_F16>(head_dim, paged, rows, modified, n_items, a, stream);
+        launch<SPD_F16>(head_dim, paged, rows, modified, tree, n_items, a, stream);
 }
 
 }  // namespace spd

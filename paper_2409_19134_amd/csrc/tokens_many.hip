@@ -77,7 +77,7 @@ constexpr float kRaise = 8.f;   // log2 of what a row's largest P may be
 template <int DT>
 constexpr float kShift = DT == SPD_F16 ? 7.f : 0.f;
 
-template <int DT, int D, bool EXACT, int MOD>
+template <int DT, int D, bool EXACT, int MOD, bool TREE>
 __global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
 {
     constexpr bool kF32 = DT == SPD_F32;
@@ -99,7 +99,7 @@ __global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
     const int my_row = min(it.row0 + wave * 32 + n, it.row0 + it.n_rows - 1);
     const int token = my_row / a.G, head = it.kv_head * a.G + (my_row - token * a.G);
     const float slope = a.score.slopes ? a.score.slopes[head] : 0.f;
-    const RowMask mask = row_mask(a.score, u, len, q_pos0 + token, token, slope);
+    const RowMask mask = token_mask<TREE>(a, u, len, q_pos0, token, slope);
     u32x4 q[KK];
     {
         const char *qr = a.q + (int64_t)(u.tok0 + token) * a.q_stride + (int64_t)head * RB + h * 16;
@@ -126,10 +126,14 @@ __global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
         mine = mine.uniform_of();
         all = all.uniform_of();
     } else {
-        auto token_of = [&](int row) { return q_pos0 + min(it.row0 + row, it.row0 + it.n_rows - 1) / a.G; };
-        mine = tile_limits(a.score, u, len, token_of(wave * 32), token_of(wave * 32 + 31));
-        all = tile_limits(a.score, u, len, token_of(0), token_of(kManyRows - 1));
+        auto token_of = [&](int row) { return min(it.row0 + row, it.row0 + it.n_rows - 1) / a.G; };
+        mine = token_limits<TREE>(a, u, len, q_pos0, token_of(wave * 32), token_of(wave * 32 + 31));
+        all = token_limits<TREE>(a, u, len, q_pos0, token_of(0), token_of(kManyRows - 1));
     }
+    add_tree<TREE>(mine, a, u, len);
+    add_tree<TREE>(all, a, u, len);
+    const int tree_begin = TREE ? plain_keys<TREE>(a, u, len) : 0;
+    auto in_tree = [&](int kt) { return TREE && a.tree.inside && kt + BN > tree_begin; };  // a tile that holds keys of the tree
     const KeyWalk walk(all, it.k_begin, k_end, BN, 1);
     const int hi = walk.hi;
 
@@ -292,7 +296,7 @@ __global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
                     x[nb][i] = fast_rcp(-1.f - fast_exp2(x[nb][i] * steep));
         } else if constexpr (MOD == kGeneral) {
             // Before all of the wave's queries a key's distance grows by one from key to key: the bias is a line, one fma per score.
-            const bool before = a.score.slopes && __builtin_amdgcn_ballot_w64(run.q < BN - 1) == 0;
+            const bool before = a.score.slopes && __builtin_amdgcn_ballot_w64(run.q < BN - 1) == 0 && !in_tree(kt);
             const float nearest = mask.slope2 * (float)(mask.dist0 - run.q);
             const float f = a.score.cap_out != 0.f ? 1.f : a.score.c;
             if (a.score.cap_out != 0.f)
@@ -311,16 +315,25 @@ __global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        x[nb][i] = biased(x[nb][i] * f, mask, run.q - (nb * 32 + 8 * (i / 4) + i % 4));
+                    for (int i = 0; i < 16; ++i) {
+                        const int key = nb * 32 + 8 * (i / 4) + i % 4;
+                        const int apart = in_tree(kt) ? tree_apart(a, u, tree_begin, mask.q_pos, kt + 4 * h + key) : run.q - key;
+                        x[nb][i] = biased(x[nb][i] * f, mask, apart);
+                    }
             }
         }
-        if (masked)
+        if (masked) {
+            uint64_t branch = 0;
+            if (in_tree(kt))
+                branch = tree_sees(a, u, tree_begin, token, mask.q_pos, kt + 4 * h, BN);
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    x[nb][i] = run.sees(mask, nb * 32 + 8 * (i / 4) + i % 4) ? x[nb][i] : -INFINITY;
+                for (int i = 0; i < 16; ++i) {
+                    const int key = nb * 32 + 8 * (i / 4) + i % 4;
+                    x[nb][i] = run.sees(mask, key) || (TREE && (branch >> key & 1u)) ? x[nb][i] : -INFINITY;
+                }
+        }
         if (MOD != kPlain || masked)
             top = top_of(x, 0, 16 * NB, -INFINITY);
         const float mt = wave_xor_max<32>(top) * c;
@@ -361,7 +374,7 @@ __global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
     auto add_nonfinite = [&](int kt) __attribute__((always_inline)) {
 #pragma unroll 1
         for (int key = kt; key <= min(kt + BN - 1, t_last); ++key) {
-            if (!sees(mask, key))
+            if (!sees(mask, key) && !(in_tree(kt) && key >= tree_begin && tree_sees(a, u, tree_begin, token, mask.q_pos, key, 1)))
                 continue;
             const char *v = v_base + token_offset(a, table, key);
 #pragma unroll
@@ -449,44 +462,49 @@ __global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
     }
 }
 
-template <int DT, int D, bool EXACT>
+template <int DT, int D, bool EXACT, bool TREE>
 void launch(bool modified, int64_t n_items, const TokArgs &a, hipStream_t stream)
 {
     const dim3 grid((unsigned)n_items), block(256);
     if (!modified)
-        hipLaunchKernelGGL((tokens_many_kernel<DT, D, EXACT, kPlain>), grid, block, 0, stream, a);
+        hipLaunchKernelGGL((tokens_many_kernel<DT, D, EXACT, kPlain, TREE>), grid, block, 0, stream, a);
     else if (!EXACT && !a.score.slopes && a.score.cap_out <= kCappedMost)
-        hipLaunchKernelGGL((tokens_many_kernel<DT, D, EXACT, EXACT ? kGeneral : kCapped>), grid, block, 0, stream, a);
+        hipLaunchKernelGGL((tokens_many_kernel<DT, D, EXACT, EXACT ? kGeneral : kCapped, TREE>), grid, block, 0, stream, a);
     else
-        hipLaunchKernelGGL((tokens_many_kernel<DT, D, EXACT, kGeneral>), grid, block, 0, stream, a);
+        hipLaunchKernelGGL((tokens_many_kernel<DT, D, EXACT, kGeneral, TREE>), grid, block, 0, stream, a);
 }
-template <int DT, int D>
+template <int DT, int D, bool TREE>
 void launch(bool modified, int64_t n_items, const TokArgs &a, hipStream_t stream)
 {
     if (DT == SPD_F32 || a.out_f32)
-        launch<DT, D, true>(modified, n_items, a, stream);
+        launch<DT, D, true, TREE>(modified, n_items, a, stream);
     else if constexpr (DT != SPD_F32)
-        launch<DT, D, false>(modified, n_items, a, stream);
+        launch<DT, D, false, TREE>(modified, n_items, a, stream);
+}
+template <int DT, int D>
+void launch(bool modified, bool tree, int64_t n_items, const TokArgs &a, hipStream_t stream)
+{
+    tree ? launch<DT, D, true>(modified, n_items, a, stream) : launch<DT, D, false>(modified, n_items, a, stream);
 }
 template <int DT>
-void launch(int head_dim, bool modified, int64_t n_items, const TokArgs &a, hipStream_t stream)
+void launch(int head_dim, bool modified, bool tree, int64_t n_items, const TokArgs &a, hipStream_t stream)
 {
     if (head_dim == 64)
-        launch<DT, 64>(modified, n_items, a, stream);
+        launch<DT, 64>(modified, tree, n_items, a, stream);
     else
-        launch<DT, 128>(modified, n_items, a, stream);
+        launch<DT, 128>(modified, tree, n_items, a, stream);
 }
 
 }  // namespace
 
-void launch_tokens_many(int dtype, int head_dim, bool modified, int64_t n_items, const TokArgs &a, hipStream_t stream)
+void launch_tokens_many(int dtype, int head_dim, bool modified, bool tree, int64_t n_items, const TokArgs &a, hipStream_t stream)
 {
     if (dtype == SPD_F32)
-        launch<SPD_F32>(head_dim, modified, n_items, a, stream);
+        launch<SPD_F32>(head_dim, modified, tree, n_items, a, stream);
     else if (dtype == SPD_BF16)
-        launch<SPD_BF16>(head_dim, modified, n_items, a, stream);
+        launch<SPD_BF16>(head_dim, modified, tree, n_items, a, stream);
     else
-        launch<SPD_F16>(head_dim, modified, n_items, a, stream);
+        launch<SPD_F16>(head_dim, modified, tree, n_items, a, stream);
 }
 
 }  // namespace spd

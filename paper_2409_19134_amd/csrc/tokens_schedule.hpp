@@ -13,6 +13,7 @@ namespace spd::host {
 
 constexpr int32_t kMaxPosition = 1 << 30;
 constexpr int64_t kMaxStrideBytes = (int64_t)1 << 28;
+constexpr int32_t kMaxLayers = 1024;  // views of one call
 
 inline bool token_stride_ok(int64_t stride, int64_t heads, int head_dim, int es)
 {
@@ -107,8 +108,20 @@ constexpr float kMaxCap = 1e30f;  // cap log2(e) stays finite, and what scale / 
 
 inline int32_t first_key_position(const spd_score *c, int u) { return c && c->k_pos ? c->k_pos[u] : 0; }
 
+// Sets of a tree's tokens: `words` of 64 bits each hold every user's tokens.
+inline int validate_tree_counts(int32_t n_users, const int32_t *n_new, int32_t words)
+{
+    if (words < 1 || words > SPD_MAX_TREE_WORDS)
+        return SPD_ERR_SHAPE;
+    for (int u = 0; u < n_users; ++u)
+        if (n_new[u] > 64 * words)
+            return SPD_ERR_LEN;
+    return SPD_OK;
+}
+
+// tree: nullptr without one.
 inline int validate_tokens(const spd_shape *s, const void *q, int64_t q_stride, const spd_kv_view *v, const int32_t *n_new, const spd_score *c,
-                           const void *out, int32_t out_dtype, const float *lse)
+                           const void *out, int32_t out_dtype, const float *lse, const spd_tree *tree = nullptr)
 {
     int rc = validate_shape(s);
     if (rc == SPD_OK)
@@ -131,6 +144,8 @@ inline int validate_tokens(const spd_shape *s, const void *q, int64_t q_stride, 
         return SPD_ERR_LEN;
     int64_t total = 0;
     rc = validate_counts(s, v, n_new, !(c && c->q_pos), &total);
+    if (rc == SPD_OK && tree)
+        rc = validate_tree_counts(v->n_users, n_new, tree->n_words);
     if (rc != SPD_OK)
         return rc;
     for (int u = 0; u < v->n_users; ++u) {
@@ -146,12 +161,113 @@ inline int validate_tokens(const spd_shape *s, const void *q, int64_t q_stride, 
         return SPD_ERR_ALIGN;
     if (total == 0)
         return SPD_OK;
-    if (!q || !out || !lse)
+    if (!q || !out || !lse || (tree && (!tree->seen || !tree->depth)))
         return SPD_ERR_NULL;
+    if (tree && ((reinterpret_cast<uintptr_t>(tree->seen) & 7u) || (reinterpret_cast<uintptr_t>(tree->depth) & 3u)))
+        return SPD_ERR_ALIGN;
     if (!aligned16(q) || !aligned16(out) || (reinterpret_cast<uintptr_t>(lse) & 3u) ||
         !token_stride_ok(q_stride, s->n_q_heads, s->head_dim, elt_size(s->dtype)))
         return SPD_ERR_ALIGN;
     return SPD_OK;
+}
+
+inline int validate_tree_plan(int32_t n_users, const int32_t *n_new, const int32_t *parents, const int32_t *first, int32_t words, const uint64_t *seen,
+                              const int32_t *depth, const int32_t *positions)
+{
+    if (n_users < 0)
+        return SPD_ERR_LEN;
+    if (n_users > 0 && !n_new)
+        return SPD_ERR_NULL;
+    int64_t total = 0;
+    for (int u = 0; u < n_users; ++u) {
+        if (n_new[u] < 0)
+            return SPD_ERR_LEN;
+        total += n_new[u];
+    }
+    if (total > 0x7fffffffll)
+        return SPD_ERR_LEN;
+    const int rc = validate_tree_counts(n_users, n_new, words);
+    if (rc != SPD_OK)
+        return rc;
+    if (total == 0)
+        return SPD_OK;
+    if (!parents || !seen || !depth || (first != nullptr) != (positions != nullptr))
+        return SPD_ERR_NULL;
+    if (first)
+        for (int u = 0; u < n_users; ++u)
+            if (first[u] < 0 || (int64_t)first[u] + n_new[u] > kMaxPosition)
+                return SPD_ERR_LEN;
+    if ((reinterpret_cast<uintptr_t>(seen) & 7u) || ((reinterpret_cast<uintptr_t>(parents) | reinterpret_cast<uintptr_t>(depth) |
+                                                       reinterpret_cast<uintptr_t>(positions)) & 3u))
+        return SPD_ERR_ALIGN;
+    return SPD_OK;
+}
+
+// Layers' views that one call takes: alike but for where their caches and block tables lie.
+inline int validate_layers(const spd_shape *s, const spd_kv_view *views, int32_t n_views)
+{
+    int rc = validate_shape(s);
+    if (rc != SPD_OK)
+        return rc;
+    if (n_views < 0 || n_views > kMaxLayers)
+        return SPD_ERR_LEN;
+    return n_views > 0 && !views ? SPD_ERR_NULL : SPD_OK;
+}
+
+inline int validate_keep(const spd_shape *s, const spd_kv_view *views, int32_t n_views, const int32_t *n_last, const int32_t *keep, const int32_t *n_keep)
+{
+    int rc = validate_layers(s, views, n_views);
+    for (int i = 0; rc == SPD_OK && i < n_views; ++i) {
+        const spd_kv_view &v = views[i], &v0 = views[0];
+        rc = validate_view(s, &v);
+        if (rc != SPD_OK || i == 0)
+            continue;
+        if (v.n_users != v0.n_users || v.block_size != v0.block_size || v.token_stride != v0.token_stride || v.head_stride != v0.head_stride ||
+            (v.block_size != 0 && v.block_stride != v0.block_stride) || (v.head_strides != nullptr) != (v0.head_strides != nullptr) ||
+            (v.k_ptrs_dev != nullptr) != (v0.k_ptrs_dev != nullptr))
+            return SPD_ERR_SHAPE;
+        for (int u = 0; u < v.n_users; ++u)
+            if (v.lens[u] != v0.lens[u] || (v.head_strides && v.block_size == 0 && v.lens[u] > 0 && v.head_strides[u] != v0.head_strides[u]))
+                return SPD_ERR_SHAPE;
+    }
+    if (rc != SPD_OK || n_views == 0)
+        return rc;
+    int64_t total = 0;
+    rc = validate_counts(s, &views[0], n_last, true, &total);
+    if (rc != SPD_OK || total == 0)
+        return rc;
+    if (!keep || !n_keep)
+        return SPD_ERR_NULL;
+    return (reinterpret_cast<uintptr_t>(keep) | reinterpret_cast<uintptr_t>(n_keep)) & 3u ? SPD_ERR_ALIGN : SPD_OK;
+}
+
+inline int validate_pages(const spd_shape *s, const spd_kv_view *views, int32_t n_views, int32_t n_pages, int32_t n_pairs, const int32_t *pairs,
+                          const int32_t *n_tokens)
+{
+    const int rc = validate_layers(s, views, n_views);
+    if (rc != SPD_OK)
+        return rc;
+    if (n_pages < 0 || n_pairs < 0)
+        return SPD_ERR_LEN;
+    const int es = elt_size(s->dtype);
+    for (int i = 0; i < n_views; ++i) {
+        const spd_kv_view &v = views[i], &v0 = views[0];
+        if (page_shift(v.block_size) < 0 || v.block_size != v0.block_size || v.token_stride != v0.token_stride || v.head_stride != v0.head_stride ||
+            v.block_stride != v0.block_stride)
+            return SPD_ERR_SHAPE;
+        if (n_pages == 0 || n_pairs == 0)
+            continue;
+        if (!v.k_pool || !v.v_pool)
+            return SPD_ERR_NULL;
+        if (!aligned16(v.k_pool) || !aligned16(v.v_pool) || v.token_stride < s->head_dim || (v.token_stride * es) % 16 != 0 || v.head_stride < 0 ||
+            (v.head_stride * es) % 16 != 0 || v.block_stride <= 0 || (v.block_stride * es) % 16 != 0)
+            return SPD_ERR_ALIGN;
+    }
+    if (n_views == 0 || n_pages == 0 || n_pairs == 0)
+        return SPD_OK;
+    if (!pairs)
+        return SPD_ERR_NULL;
+    return (reinterpret_cast<uintptr_t>(pairs) & 7u) || (reinterpret_cast<uintptr_t>(n_tokens) & 3u) ? SPD_ERR_ALIGN : SPD_OK;
 }
 
 // A user of a call as the schedule sees it: positions relative to the view's first key.
@@ -318,8 +434,9 @@ inline int64_t stretch_steps(const std::vector<TokTile> &tiles, int64_t at_once,
 
 constexpr int kXcds = 8;
 
+// tree: a user's tokens lie at any depth, in any order, so every tile's rows may see what any of the user's can.
 inline void build_tok_tables(const spd_shape *s, const spd_kv_view *v, const std::vector<TokUserPlan> &plan, int causal, int window, int n_cus,
-                             TokTables &T)
+                             TokTables &T, bool tree = false)
 {
     const int G = s->n_q_heads / s->n_kv_heads, Hkv = s->n_kv_heads, es = elt_size(s->dtype);
     const bool addresses = v->block_size == 0 && !v->k_ptrs_dev;
@@ -356,7 +473,7 @@ inline void build_tok_tables(const spd_shape *s, const spd_kv_view *v, const std
         const int step = k == TokKernel::kMany ? many_keys(s->dtype) : kFewKeys, cap = tile_rows(k);
         for (int64_t r0 = 0; r0 < rows; r0 += cap) {
             const int64_t r1 = std::min<int64_t>(rows, r0 + cap);
-            const TokSpan span = tile_span(p, causal, window, (int)(r0 / G), (int)((r1 - 1) / G));
+            const TokSpan span = tree ? tile_span(p, causal, window, 0, p.n_tok - 1) : tile_span(p, causal, window, (int)(r0 / G), (int)((r1 - 1) / G));
             T.growable = T.growable && span.hi == p.len;
             spans.emplace_back(span, step);
             for (int h = 0; h < Hkv; ++h)
