@@ -4,6 +4,10 @@
 
 namespace spd {
 
+typedef __attribute__((address_space(1))) char global_char;  // (an address that came from memory: not one of LDS)
+typedef __attribute__((address_space(1))) u32x4 global_u32x4;
+typedef __attribute__((address_space(1))) const int32_t global_i32;
+
 struct KeepUser {
     int64_t head_stride;      // bytes
     int32_t user, token;      // its number, and its first entry of the list
@@ -27,69 +31,80 @@ struct KeepArgs {
     int64_t token_stride, block_stride;  // bytes
     int32_t max_blocks, page_shift;
     int32_t n_heads, n_layers, slices;
-    uint32_t first, n_waves;             // the launch's first wave's number, and how many there are
+    uint32_t first, n_streams;           // the launch's first stream's number, and how many there are
 };
 
-// Tokens kept, in place.  A wave has a slice of the channels of one head of K or V of one user and layer to itself and goes through the kept tokens in
-// order, some at a time: all of them are read before any is written.  Place i gets what lay at keep[i] >= i: later entries read at or behind their own
-// places, so never where earlier ones have written, and nothing has to be asked of other waves.
-template <int RB, bool PAGED>
-__global__ __launch_bounds__(256) void keep_kernel(const KeepArgs a, const KeepUsers users, const KeepLayers layers)
+// Tokens kept, in place.  A stream is a slice of the channels of one head of K or V of one user and layer.  WAVES waves have it to themselves and go through
+// the kept tokens in order, some at a time: all of them are read before any is written.  Place i gets what lay at keep[i] >= i: later entries
+// are read at or behind their own places, so never where earlier ones were written, and nothing has to be asked of other workgroups.
+template <int RB, bool PAGED, int WAVES>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void keep_kernel(const KeepArgs a, const KeepUsers users, const KeepLayers layers)
 {
-    constexpr int kLoads = 8;
-    const int lane = threadIdx.x & 63;
-    uint32_t id = a.first + blockIdx.x * 4u + (uint32_t)uniform((int)(threadIdx.x >> 6));
-    if (id >= a.n_waves)
+    constexpr int kLoads = WAVES == 1 ? (RB > 256 ? 4 : 2) : 8;
+    const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
+    uint32_t id = a.first + (WAVES == 1 ? blockIdx.x * 4u + (uint32_t)wave : blockIdx.x);
+    int slice;
+    if constexpr (WAVES == 1) {
+        slice = (int)(id % (uint32_t)a.slices);
+        id /= (uint32_t)a.slices;
+    } else {  // (workgroups i and i + 8 run on one XCD: the slices of a cache line meet in its L2)
+        const uint32_t eight = id / (8u * (uint32_t)a.slices), in = id - eight * 8u * (uint32_t)a.slices;
+        slice = (int)(in / 8u);
+        id = eight * 8u + in % 8u;
+    }
+    if (id >= a.n_streams)
         return;
-    const int slice = (int)(id % (uint32_t)a.slices);
-    id /= (uint32_t)a.slices;
     const int head = (int)(id % (uint32_t)a.n_heads);
     id /= (uint32_t)a.n_heads;
     const int kv = (int)(id & 1u);
     id >>= 1;
     const KeepLayer &layer = layers.it[id % (uint32_t)a.n_layers];
-    const KeepUser &u = users.it[id / (uint32_t)a.n_layers];
-    const int count = min(max(a.n_keep[u.user], 0), u.n);
-    char *base;
-    const int32_t *table = nullptr;
-    if constexpr (PAGED) {
-        base = layer.kv[kv];
-        table = layer.table + (int64_t)u.user * a.max_blocks;
-    } else {
-        base = reinterpret_cast<char *const *>(layer.kv[kv])[u.user];
-    }
+    const KeepUser u = users.it[id / (uint32_t)a.n_layers];
+    const int count = uniform(min(max(a.n_keep[u.user], 0), u.n));
     const int pieces = RB / 16 / a.slices, rows = 64 / pieces;  // sixteen bytes to a lane; tokens to a load
-    base += head * u.head_stride + (slice * pieces + lane % pieces) * 16;
-    const int mine = lane / pieces;
+    const int64_t lane_off = head * u.head_stride + (slice * pieces + lane % pieces) * 16;
+    global_char *base;
+    global_i32 *table = nullptr, *const keep = (global_i32 *)(a.keep + u.token);
+    if constexpr (PAGED) {
+        base = (global_char *)layer.kv[kv] + lane_off;
+        table = (global_i32 *)(layer.table + (int64_t)u.user * a.max_blocks);
+    } else {
+        base = (global_char *)reinterpret_cast<char *const *>(layer.kv[kv])[u.user] + lane_off;
+    }
+    const int mine = (WAVES == 1 ? 0 : wave * rows) + lane / pieces, step = rows * (WAVES == 1 ? 1 : WAVES);
     auto at = [&](int place) __attribute__((always_inline)) {
         if constexpr (PAGED)
             return (int64_t)table[place >> a.page_shift] * a.block_stride + (int64_t)(place & ((1 << a.page_shift) - 1)) * a.token_stride;
         else
             return (int64_t)place * a.token_stride;
     };
-    for (int i0 = 0; i0 < count; i0 += rows * kLoads) {
-        u32x4 w[kLoads];
-        int from[kLoads];
+    auto entries = [&](int i0, int (&from)[kLoads]) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
-            const int i = i0 + j * rows + mine;
-            int k = -1;
-            if (i < count) {
-                k = a.keep[u.token + i];
-                if (k <= i || k >= u.n)  // in place already, or no such token
-                    k = -1;
-            }
-            from[j] = k;
+            const int i = i0 + j * step + mine;
+            const int k = i < count ? keep[i] : -1;
+            from[j] = k > i && k < u.n ? k : -1;  // (else in place already, or no such token)
         }
+    };
+    int from[kLoads];
+    entries(0, from);
+    for (int i0 = 0; i0 < count; i0 += step * kLoads) {
+        u32x4 w[kLoads];
 #pragma unroll
         for (int j = 0; j < kLoads; ++j)
             if (from[j] >= 0)
-                w[j] = *reinterpret_cast<const u32x4 *>(base + at(u.begin + from[j]));
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // all lanes' reads are back before the first write
+                w[j] = *(global_u32x4 *)(base + at(u.begin + from[j]));
+        int next[kLoads];
+        entries(i0 + step * kLoads, next);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the wave's reads are back before the first write ...
+        if constexpr (WAVES > 1)
+            __syncthreads();  // ... and all waves'
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j)
+        for (int j = 0; j < kLoads; ++j) {
             if (from[j] >= 0)
-                *reinterpret_cast<u32x4 *>(base + at(u.begin + i0 + j * rows + mine)) = w[j];
+                *(global_u32x4 *)(base + at(u.begin + i0 + j * step + mine)) = w[j];
+            from[j] = next[j];
+        }
     }
 }
 
@@ -103,10 +118,11 @@ struct PageArgs {
     int32_t n_pages, n_heads, n_layers, page_shift, token_major, parts;
     uint32_t first;                      // the launch's first workgroup's number
 };
-constexpr int kPageLoads = 8, kPagePieces = 256 * kPageLoads;  // sixteen bytes each, of a workgroup
 
-// Pages copied: a workgroup takes 32 KB of a page of K or V in one layer.
-template <int RB>
+// Pages copied: a workgroup takes so much of a page of K or V in one layer as its threads hold in kPageLoads pieces of sixteen bytes.
+// DENSE: a page's bytes lie end to end, tokens in order (or whole pages in any order).  ONCE: past the caches.
+constexpr int kPageLoads = 1, kPagePieces = 256 * kPageLoads;
+template <int RB, bool DENSE, bool ONCE>
 __global__ __launch_bounds__(256) void copy_pages_kernel(const PageArgs a, const PageLayers layers)
 {
     constexpr int C = RB / 16;
@@ -117,27 +133,52 @@ __global__ __launch_bounds__(256) void copy_pages_kernel(const PageArgs a, const
     id >>= 1;
     char *const pool = layers.kv[id % (uint32_t)a.n_layers][kv];
     const uint32_t pair = id / (uint32_t)a.n_layers;
-    const int from = a.pairs[2 * pair], to = a.pairs[2 * pair + 1];
+    const int from = uniform(a.pairs[2 * (size_t)pair]), to = uniform(a.pairs[2 * (size_t)pair + 1]);
     if ((unsigned)from >= (unsigned)a.n_pages || (unsigned)to >= (unsigned)a.n_pages || from == to)
         return;
-    const int page = 1 << a.page_shift, n = a.n_tokens ? min(max(a.n_tokens[pair], 0), page) : page;
+    const int page = 1 << a.page_shift, n = a.n_tokens ? uniform(min(max(a.n_tokens[pair], 0), page)) : page;
     const char *const src = pool + from * a.block_stride;
     char *const dst = pool + to * a.block_stride;
+    const int first = part * kPagePieces + (int)threadIdx.x;
     u32x4 w[kPageLoads];
-    int64_t off[kPageLoads];
+    auto load = [](const char *p) __attribute__((always_inline)) {
+        if constexpr (ONCE)
+            return __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p));
+        else
+            return *reinterpret_cast<const u32x4 *>(p);
+    };
+    auto store = [](char *p, u32x4 v) __attribute__((always_inline)) {
+        if constexpr (ONCE)
+            __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(p));
+        else
+            *reinterpret_cast<u32x4 *>(p) = v;
+    };
+    if constexpr (DENSE) {
+        const int pieces = n * a.n_heads * C;
 #pragma unroll
-    for (int j = 0; j < kPageLoads; ++j) {
-        const int i = part * kPagePieces + j * 256 + (int)threadIdx.x, row = i / C;
-        const int token = a.token_major ? row / a.n_heads : row & (page - 1);
-        const int head = a.token_major ? row - token * a.n_heads : row >> a.page_shift;
-        off[j] = token < n && head < a.n_heads ? token * a.token_stride + head * a.head_stride + i % C * 16 : -1;
-        if (off[j] >= 0)
-            w[j] = *reinterpret_cast<const u32x4 *>(src + off[j]);
+        for (int j = 0; j < kPageLoads; ++j)
+            if (first + j * 256 < pieces)
+                w[j] = load(src + (int64_t)(first + j * 256) * 16);
+#pragma unroll
+        for (int j = 0; j < kPageLoads; ++j)
+            if (first + j * 256 < pieces)
+                store(dst + (int64_t)(first + j * 256) * 16, w[j]);
+    } else {
+        int64_t off[kPageLoads];
+#pragma unroll
+        for (int j = 0; j < kPageLoads; ++j) {
+            const int i = first + j * 256, row = i / C;
+            const int token = a.token_major ? row / a.n_heads : row & (page - 1);
+            const int head = a.token_major ? row - token * a.n_heads : row >> a.page_shift;
+            off[j] = token < n && head < a.n_heads ? token * a.token_stride + head * a.head_stride + i % C * 16 : -1;
+            if (off[j] >= 0)
+                w[j] = load(src + off[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < kPageLoads; ++j)
+            if (off[j] >= 0)
+                store(dst + off[j], w[j]);
     }
-#pragma unroll
-    for (int j = 0; j < kPageLoads; ++j)
-        if (off[j] >= 0)
-            *reinterpret_cast<u32x4 *>(dst + off[j]) = w[j];
 }
 
 }  // namespace spd

@@ -16,7 +16,8 @@ struct TokUser {
     int32_t q_pos;                // position of its first new token (grows with grow_q)
     int32_t prefix;               // keys below it are seen by every query
     int32_t k_pos;                // position of key 0, for the ranges
-    int32_t pad[4];
+    int32_t next;                 // (in a TreeItem)
+    int32_t pad[3];
 };
 static_assert(sizeof(TokUser) == 64);
 
@@ -29,6 +30,14 @@ struct TokItem {
     int32_t to_len;          // 1: k_end is the view's length (grows with it)
 };
 static_assert(sizeof(TokItem) == 32);
+
+// The same with its user beside it, for trees: one read brings all that a workgroup needs to ask for keys.  A workgroup takes several, one after the other: the
+// first is the one with its number, and each names the next.
+struct TreeItem {
+    TokItem it;
+    TokUser u;  // u.next: the item after this one, 0: none
+};
+static_assert(sizeof(TreeItem) == 96);
 
 // A tile whose keys were split: partials slot .. slot + n_chunks - 1.
 struct TokJoin {
@@ -73,6 +82,7 @@ struct TokArgs {
     float2 *part_lse; // [slot][rows of a tile]: log2 of the sum, and what the final lse adds to it (natural log)
     ScoreArgs score;
     TreeArgs tree;    // the kernels' tree form
+    int32_t first_piece;    // ... its items are TreeItems, and the launch's first workgroup's is the first_piece-th
 };
 
 // A query row's masks and bias (slope: its head's, 0 without).  It sees the keys in [mlo, mlo + mn) and in [plo, plo + pn).
@@ -265,8 +275,8 @@ __device__ __forceinline__ void add_tree(Limits &l, const TokArgs &a, const TokU
         l.full_hi = min(l.full_hi, base);
     }
 }
-// Which of the `n` (up to 64) keys from `key` on a tree's token sees as tokens of the tree, which begins at key `base`.
-__device__ __forceinline__ uint64_t tree_sees(const TokArgs &a, const TokUser &u, int base, int token, int q_pos, int key, int n)
+// Which of the 64 keys from `key` on are tokens of the tree, which begins at key `base`, that are in a token's set.
+__device__ __forceinline__ uint64_t tree_bits(const TokArgs &a, const TokUser &u, int base, int token, int key)
 {
     const int first = key - base, word = first >> 6, shift = first & 63;
     const uint64_t *const set = a.tree.seen + (int64_t)(u.tok0 + token) * a.tree.words;
@@ -275,28 +285,34 @@ __device__ __forceinline__ uint64_t tree_sees(const TokArgs &a, const TokUser &u
         bits = set[word] >> shift;
     if (shift && (unsigned)(word + 1) < (unsigned)a.tree.words)
         bits |= set[word + 1] << (64 - shift);
-    const int left = min(n, u.n_tok - first);  // (bits behind the last token mean nothing)
-    bits &= left >= 64 ? ~0ull : left > 0 ? (1ull << left) - 1 : 0ull;
-    // windows shorter than the tree may be deep, and documents
-    if (a.score.ranges || (a.score.window && a.score.window < u.n_tok)) {
-        int lo = 0, hi = 0x7fffffff;
+    const int left = u.n_tok - first;  // (bits behind the last token mean nothing)
+    return left >= 64 ? bits : left > 0 ? bits & ((1ull << left) - 1) : 0ull;
+}
+// The position of a key, which may be one of the tree's (or lie behind them).
+__device__ __forceinline__ int tree_position(const TokArgs &a, const TokUser &u, int base, int key)
+{
+    return key < base ? key : base + tree_depth(a, u, min(key - base, u.n_tok - 1));
+}
+// What windows shorter than the tree may be deep, and documents, leave of a token's set.
+__device__ __forceinline__ bool tree_is_cut(const TokArgs &a, const TokUser &u) { return a.score.ranges || (a.score.window && a.score.window < u.n_tok); }
+struct TreeCut {
+    int lo = 0, hi = 0x7fffffff, window = 0x7fffffff;
+    __device__ __forceinline__ TreeCut(const TokArgs &a, const TokUser &u, int token)
+    {
         if (a.score.ranges) {
             const int2 v = reinterpret_cast<const int2 *>(a.score.ranges)[u.tok0 + token];
             lo = max(v.x, 0) - u.k_pos;
             hi = max(v.y, 0) - u.k_pos;
         }
-        for (uint64_t rest = bits; rest; rest &= rest - 1) {
-            const int pos = base + tree_depth(a, u, first + __builtin_ctzll(rest));
-            if (pos < lo || pos >= hi || (a.score.window && abs(q_pos - pos) >= a.score.window))
-                bits &= ~(rest & -rest);
-        }
+        if (a.score.window)
+            window = a.score.window;
     }
-    return bits;
-}
-// The distance of a query to a key, which may be one of the tree's.
-__device__ __forceinline__ int tree_apart(const TokArgs &a, const TokUser &u, int base, int q_pos, int key)
+    __device__ __forceinline__ bool leaves(int q_pos, int pos) const { return pos >= lo && pos < hi && abs(q_pos - pos) < window; }
+};
+// All of it for one key.
+__device__ __forceinline__ bool tree_sees(const TokArgs &a, const TokUser &u, int base, int token, int q_pos, int key)
 {
-    return q_pos - (key < base ? key : base + tree_depth(a, u, min(key - base, u.n_tok - 1)));
+    return key >= base && (tree_bits(a, u, base, token, key) & 1u) && TreeCut(a, u, token).leaves(q_pos, tree_position(a, u, base, key));
 }
 
 // A row's view of a run of keys from key0 on, made anew for every run: without the detour the compiler keeps every key's differences to the row's
@@ -432,6 +448,12 @@ __attribute__((visibility("hidden"))) void launch_tokens_many(int dtype, int hea
                                                               const TokArgs &a, hipStream_t stream);
 constexpr int kManyRows = 128;  // rows of a tile of the many kernel
 __host__ __device__ constexpr int many_keys(int dtype) { return dtype == SPD_F32 ? 32 : 64; }  // keys of its steps
+// Workgroups of the few kernel's tree form that fit on a compute unit, by its rows.
+__host__ __device__ constexpr int tree_resident(int dtype, int head_dim, int rows)
+{
+    const bool f32 = dtype == SPD_F32, small = head_dim == 64;
+    return rows == 16 ? (f32 ? (small ? 3 : 2) : small ? 4 : 3) : (!f32 && small ? 3 : 2);
+}
 constexpr int kFewKeys = 32;    // keys that the few kernel's stretches are multiples of
 
 }  // namespace spd

@@ -409,7 +409,7 @@ int find_or_build(ContextBase *ctx, TokensState *t, const spd_shape *s, const sp
     size_t bytes = padded(T.users.size() * sizeof(TokUser)), off_items[kTokKernels], off_joins[kTokKernels];
     for (int k = 0; k < kTokKernels; ++k) {
         off_items[k] = bytes;
-        bytes += padded(T.items[k].size() * sizeof(TokItem));
+        bytes += padded(tree ? T.tree[k].size() * sizeof(TreeItem) : T.items[k].size() * sizeof(TokItem));
         off_joins[k] = bytes;
         bytes += padded(T.joins[k].size() * sizeof(TokJoin));
     }
@@ -424,10 +424,11 @@ int find_or_build(ContextBase *ctx, TokensState *t, const spd_shape *s, const sp
     copy(0, T.users);
     for (int k = 0; k < kTokKernels; ++k) {
         copy(off_items[k], T.items[k]);
+        copy(off_items[k], T.tree[k]);  // (one of the two)
         copy(off_joins[k], T.joins[k]);
         e->off_items[k] = off_items[k];
         e->off_joins[k] = off_joins[k];
-        e->n_items[k] = (int64_t)T.items[k].size();
+        e->n_items[k] = tree ? T.pieces[k] : (int64_t)T.items[k].size();
         e->n_joins[k] = (int64_t)T.joins[k].size();
         e->slots[k] = T.slots[k];
         e->join_rows[k] = e->join_chunks[k] = 0;
@@ -576,7 +577,8 @@ int attend(ContextBase *ctx, const spd_shape *s, const void *q, int64_t q_stride
         a.part_o = t->part + rows[k] * (size_t)s->head_dim;
         a.part_lse = part_lse + rows[k];
         in_parts(e->n_items[k], [&](int64_t first, unsigned n) {
-            a.items = items + first;
+            a.items = tree ? items : items + first;
+            a.first_piece = (int32_t)first;
             if (k == (int)TokKernel::kMany)
                 launch_tokens_many(s->dtype, s->head_dim, modified, tree != nullptr, n, a, stream);
             else
@@ -798,7 +800,8 @@ int tree_plan(ContextBase *ctx, int32_t n_users, const int32_t *n_new, const int
         if (most <= 64)
             hipLaunchKernelGGL(plan_small_kernel, dim3((unsigned)n), dim3(64), 0, stream, a, users);
         else
-            hipLaunchKernelGGL(plan_kernel, dim3((unsigned)n), dim3(kPlanThreads), 0, stream, a, users);
+            hipLaunchKernelGGL(most * words <= 4096 ? plan_kernel<4096> : plan_kernel<64 * SPD_MAX_TREE_WORDS * SPD_MAX_TREE_WORDS>, dim3((unsigned)n),
+                               dim3(kPlanThreads), 0, stream, a, users);
         n = most = 0;
         SPD_TRY(ctx, hipGetLastError());
         return SPD_OK;
@@ -889,24 +892,26 @@ int keep_tokens(ContextBase *ctx, const spd_shape *s, const spd_kv_view *views, 
     a.page_shift = paged ? page_shift(v.block_size) : 0;
     a.n_heads = s->n_kv_heads;
     const int row_bytes = s->head_dim * es;
+    const int32_t longest = *std::max_element(n_last, n_last + U);
+    const int waves = longest <= 64 ? 1 : longest <= 512 ? 4 : 16;
     KeepUsers users;
     KeepLayers layers;
     int failed = SPD_OK;
     auto launch = [&](int n_users, int n_layers) {
         const int64_t streams = (int64_t)n_users * n_layers * 2 * s->n_kv_heads;
+        a.slices = 1;
+        while (a.slices * 64 < row_bytes && streams * a.slices * waves < 8 * (int64_t)ctx->n_cus)
+            a.slices *= 2;
+        a.n_streams = (uint32_t)streams;
+        a.n_layers = n_layers;
+        const int threads = std::max(256, 64 * waves), per_group = threads / 64 / waves;
         with_row_bytes(row_bytes, [&](auto rb) {
-            // enough waves to fill the device, down to a quarter of the row's cache line to a wave
-            a.slices = 1;
-            while (a.slices * 64 < rb() && streams * a.slices < 8 * (int64_t)ctx->n_cus)
-                a.slices *= 2;
-            in_parts((streams * a.slices + 3) / 4, [&](int64_t first, unsigned n) {
-                a.first = (uint32_t)(first * 4);
-                a.n_waves = (uint32_t)(streams * a.slices);
-                a.n_layers = n_layers;
-                if (paged)
-                    hipLaunchKernelGGL((keep_kernel<rb(), true>), dim3(n), dim3(256), 0, stream, a, users, layers);
-                else
-                    hipLaunchKernelGGL((keep_kernel<rb(), false>), dim3(n), dim3(256), 0, stream, a, users, layers);
+            auto kernel = waves == 1 ? (paged ? keep_kernel<rb(), true, 1> : keep_kernel<rb(), false, 1>)
+                          : waves == 4 ? (paged ? keep_kernel<rb(), true, 4> : keep_kernel<rb(), false, 4>)
+                                       : (paged ? keep_kernel<rb(), true, 16> : keep_kernel<rb(), false, 16>);
+            in_parts(((waves == 1 ? streams : (streams + 7) / 8 * 8) * a.slices + per_group - 1) / per_group, [&](int64_t first, unsigned n) {
+                a.first = (uint32_t)(first * per_group);
+                hipLaunchKernelGGL(kernel, dim3(n), dim3((unsigned)threads), 0, stream, a, users, layers);
             });
         });
         const hipError_t e = hipGetLastError();
@@ -971,6 +976,10 @@ int copy_pages(ContextBase *ctx, const spd_shape *s, const spd_kv_view *views, i
     a.page_shift = page_shift(v.block_size);
     a.token_major = v.head_stride < v.token_stride;
     a.parts = (int32_t)(((int64_t)s->n_kv_heads * v.block_size * (row_bytes / 16) + kPagePieces - 1) / kPagePieces);
+    // a page's bytes end to end: tokens in order, or, where pages are copied whole, heads in order
+    const int64_t d = s->head_dim, H = s->n_kv_heads;
+    const bool dense = (v.head_stride == d && v.token_stride == H * d) || (!n_tokens && v.token_stride == d && v.head_stride == v.block_size * d);
+    const bool once = (int64_t)n_pairs * n_views * 2 * v.block_size * H * row_bytes >= kOnceBytes;
     PageLayers layers;
     for (int i = 0; i < n_views; i += kPageLayers) {
         const int n_layers = std::min(n_views - i, kPageLayers);
@@ -981,12 +990,14 @@ int copy_pages(ContextBase *ctx, const spd_shape *s, const spd_kv_view *views, i
         a.n_layers = n_layers;
         const int64_t groups = (int64_t)n_layers * 2 * a.parts, most = std::max<int64_t>(1, kMostGroups / groups);  // of a pair; pairs of a launch
         with_row_bytes(row_bytes, [&](auto rb) {
+            auto kernel = dense ? (once ? copy_pages_kernel<rb(), true, true> : copy_pages_kernel<rb(), true, false>)
+                                : (once ? copy_pages_kernel<rb(), false, true> : copy_pages_kernel<rb(), false, false>);
             for (int64_t p = 0; p < n_pairs; p += most) {
                 a.pairs = pairs + 2 * p;
                 a.n_tokens = n_tokens ? n_tokens + p : nullptr;
                 in_parts(groups * std::min(most, n_pairs - p), [&](int64_t first, unsigned n) {
                     a.first = (uint32_t)first;
-                    hipLaunchKernelGGL((copy_pages_kernel<rb()>), dim3(n), dim3(256), 0, stream, a, layers);
+                    hipLaunchKernelGGL(kernel, dim3(n), dim3(256), 0, stream, a, layers);
                 });
             }
         });

@@ -93,8 +93,9 @@ __device__ __forceinline__ void keep_finite(VRow<512> &v)
     }
 }
 
+// One item: a tile's rows over a stretch of keys.
 template <int DT, int D, bool PAGED, int NT, bool MOD, bool TREE>
-__global__ __launch_bounds__(256, 2) void tokens_few_kernel(const TokArgs a)
+__device__ __forceinline__ void few_item(const TokArgs &a, const TokItem &it, const TokUser &u)
 {
     constexpr int kBytes = Elt<DT>::kBytes, RB = D * kBytes, NA = step_tiles(RB), NE = 4 * NA, kStep = 16 * NA, CP = D / 16;
     constexpr int kRows = 16 * NT;
@@ -102,9 +103,10 @@ __global__ __launch_bounds__(256, 2) void tokens_few_kernel(const TokArgs a)
     __shared__ __attribute__((aligned(16))) float stage[4][16][kPitch];
     __shared__ float stage_ml[2][4][kRows];
 
-    const TokItem it = scalar_load(a.items, blockIdx.x);
-    const TokUser u = scalar_load(a.users, it.user);
-    const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
+    int tid = threadIdx.x;
+    if constexpr (TREE)  // (made anew for every item: what follows from a lane's number has no registers of its own across them)
+        asm volatile("" : "+v"(tid));
+    const int lane = tid & 63, wave = uniform(tid >> 6);
     const int r = lane & 15, grp = lane >> 4;
     const int len = u.len + a.grow_len, q_pos0 = u.q_pos + a.grow_q;
     const int k_end = it.k_end + (it.to_len ? a.grow_len : 0);
@@ -201,6 +203,12 @@ __global__ __launch_bounds__(256, 2) void tokens_few_kernel(const TokArgs a)
         load_tile<RB, NA, PAGED, false>(T, L, tb, t_last, P, walk.next(tb) - tb);
         const bool masked = tb < full_lo || tb + kStep > full_hi;
         const int t0 = tb + grp * NE;
+        const bool in_tree = TREE && a.tree.inside && tb + kStep > tree_begin;
+        int pos[TREE ? NE : 1];  // of a step with keys of the tree
+        if (TREE && in_tree)
+#pragma unroll
+            for (int e = 0; e < NE; ++e)
+                pos[e] = tree_position(a, u, tree_begin, t0 + e);
         float p[NT][NE];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -231,19 +239,23 @@ __global__ __launch_bounds__(256, 2) void tokens_few_kernel(const TokArgs a)
             float x[NE];
             const RunMask run(mask[nt], t0);
 #pragma unroll
-            for (int e = 0; e < NE; ++e) {
-                int apart = run.q - e;
-                if (TREE && MOD && a.score.slopes && tb + kStep > tree_begin && a.tree.inside)
-                    apart = tree_apart(a, u, tree_begin, mask[nt].q_pos, t0 + e);
-                x[e] = modified<MOD>(s[e / 4][e % 4], a.score, mask[nt], apart);
-            }
-            if (masked) {
-                uint32_t branch = 0;
-                if (TREE && tb + kStep > tree_begin && a.tree.inside)
-                    branch = (uint32_t)tree_sees(a, u, tree_begin, token[nt], mask[nt].q_pos, t0, NE);
+            for (int e = 0; e < NE; ++e)
+                x[e] = modified<MOD>(s[e / 4][e % 4], a.score, mask[nt], TREE && in_tree ? mask[nt].q_pos - pos[e] : run.q - e);
+            if (TREE && in_tree) {
+                uint32_t branch = (uint32_t)tree_bits(a, u, tree_begin, token[nt], t0);
+                if (tree_is_cut(a, u)) {
+                    const TreeCut cut(a, u, token[nt]);
+#pragma unroll
+                    for (int e = 0; e < NE; ++e)
+                        branch &= cut.leaves(mask[nt].q_pos, pos[e]) ? ~0u : ~(1u << e);
+                }
 #pragma unroll
                 for (int e = 0; e < NE; ++e)
-                    x[e] = run.sees(mask[nt], e) || (TREE && (branch >> e & 1u)) ? x[e] : -INFINITY;
+                    x[e] = run.sees(mask[nt], e) || (branch >> e & 1u) ? x[e] : -INFINITY;
+            } else if (masked) {
+#pragma unroll
+                for (int e = 0; e < NE; ++e)
+                    x[e] = run.sees(mask[nt], e) ? x[e] : -INFINITY;
             }
             float mt = x[0];
 #pragma unroll
@@ -300,8 +312,7 @@ __global__ __launch_bounds__(256, 2) void tokens_few_kernel(const TokArgs a)
                 const char *v = L.v_base + token_offset(a, L.bt_row, key);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    if (!sees(mask[nt], key) &&
-                        !(TREE && a.tree.inside && key >= tree_begin && tree_sees(a, u, tree_begin, token[nt], mask[nt].q_pos, key, 1)))
+                    if (!sees(mask[nt], key) && !(TREE && in_tree && tree_sees(a, u, tree_begin, token[nt], mask[nt].q_pos, key)))
                         continue;
 #pragma unroll
                     for (int cc = 0; cc < CP; ++cc)
@@ -337,7 +348,7 @@ __global__ __launch_bounds__(256, 2) void tokens_few_kernel(const TokArgs a)
         constexpr int kQuads = D / 4;  // a row's results, four channels to a thread
 #pragma unroll
         for (int j = 0; j < 16 * kQuads / 256; ++j) {
-            const int idx = j * 256 + (int)threadIdx.x, rr = idx / kQuads, ch = idx % kQuads * 4;
+            const int idx = j * 256 + tid, rr = idx / kQuads, ch = idx % kQuads * 4;
             if (nt * 16 + rr >= it.n_rows)
                 continue;
             float m = stage_ml[0][0][nt * 16 + rr];
@@ -375,6 +386,26 @@ __global__ __launch_bounds__(256, 2) void tokens_few_kernel(const TokArgs a)
                     a.lse[at] = lse2 * kLn2 + offset;
             }
         }
+    }
+}
+
+template <int DT, int D, bool PAGED, int NT, bool MOD, bool TREE>
+__global__ __launch_bounds__(256, TREE ? tree_resident(DT, D, 16 * NT) : 2) void tokens_few_kernel(const TokArgs a)
+{
+    if constexpr (TREE) {
+        int i = a.first_piece + (int)blockIdx.x;
+        do {
+            const TreeItem x = scalar_load(reinterpret_cast<const TreeItem *>(a.items), i);
+            if (x.it.n_rows != 0)  // (else it fills up the launch order)
+                few_item<DT, D, PAGED, NT, MOD, TREE>(a, x.it, x.u);
+            i = x.u.next;
+            if (i != 0)
+                __syncthreads();  // (LDS is written anew)
+        } while (i != 0);
+    } else {
+        const TokItem it = scalar_load(a.items, blockIdx.x);
+        const TokUser u = scalar_load(a.users, it.user);
+        few_item<DT, D, PAGED, NT, MOD, TREE>(a, it, u);
     }
 }
 

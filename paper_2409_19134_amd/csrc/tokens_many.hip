@@ -50,6 +50,7 @@ struct Block<SPD_F32> {
 };
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) char lds_char;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
@@ -77,38 +78,61 @@ constexpr float kRaise = 8.f;   // log2 of what a row's largest P may be
 template <int DT>
 constexpr float kShift = DT == SPD_F16 ? 7.f : 0.f;
 
+template <int DT, int D>
+struct Tiles {
+    static constexpr int kBytes = many_keys(DT) * D * (DT == SPD_F32 ? 4 : 2);
+    char (*k)[kBytes], (*v)[kBytes];  // two buffers of each, in LDS
+};
+
+// One item: a tile's rows over a stretch of keys.
 template <int DT, int D, bool EXACT, int MOD, bool TREE>
-__global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
+__device__ __forceinline__ void many_item(const TokArgs &a, const TokItem &it, const TokUser &u, const Tiles<DT, D> lds)
 {
     constexpr bool kF32 = DT == SPD_F32;
     constexpr int kBytes = kF32 ? 4 : 2, RB = D * kBytes, BN = many_keys(DT), NB = BN / 32, C = RB / 16, KK = RB / 32, CB = D / 32;
-    constexpr int kTile = BN * RB, kPieces = BN * C / 256;
+    constexpr int kPieces = BN * C / 256;
     constexpr int kTerms = EXACT ? Block<DT>::kTerms : 1;
-    __shared__ __attribute__((aligned(16))) char k_lds[2][kTile], v_lds[2][kTile];
-
-    const TokItem it = scalar_load(a.items, blockIdx.x);
-    if (it.n_rows == 0)
-        return;  // (fills up the launch order)
-    const TokUser u = scalar_load(a.users, it.user);
+    auto &k_lds = lds.k;
+    auto &v_lds = lds.v;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int n = lane & 31, h = lane >> 5;
     const int len = u.len + a.grow_len, q_pos0 = u.q_pos + a.grow_q;
     const int k_end = it.k_end + (it.to_len ? a.grow_len : 0);
 
     // the lane's row, its query and masks (rows behind the last repeat it and are not stored)
-    const int my_row = min(it.row0 + wave * 32 + n, it.row0 + it.n_rows - 1);
-    const int token = my_row / a.G, head = it.kv_head * a.G + (my_row - token * a.G);
+    // (In the tree form worked out anew where it is needed again: the loop has no registers for it.)
+    struct Place {
+        int token, head;
+    };
+    auto place = [&](int lane_) __attribute__((always_inline)) {
+        const int my_row = min(it.row0 + wave * 32 + (lane_ & 31), it.row0 + it.n_rows - 1), token_ = my_row / a.G;
+        return Place{token_, it.kv_head * a.G + (my_row - token_ * a.G)};
+    };
+    const Place mine_ = place(lane);
+    const int token = mine_.token, head = mine_.head;
+    auto place_again = [&]() __attribute__((always_inline)) {
+        if constexpr (!TREE)
+            return mine_;
+        int l = lane;
+        asm volatile("" : "+v"(l));
+        return place(l);
+    };
     const float slope = a.score.slopes ? a.score.slopes[head] : 0.f;
-    const RowMask mask = token_mask<TREE>(a, u, len, q_pos0, token, slope);
+    RowMask mask;
     u32x4 q[KK];
-    {
+    auto read_row = [&]() __attribute__((always_inline)) {
+        mask = token_mask<TREE>(a, u, len, q_pos0, token, slope);
         const char *qr = a.q + (int64_t)(u.tok0 + token) * a.q_stride + (int64_t)head * RB + h * 16;
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk)
 #pragma unroll
             for (int j = 0; j < 4; ++j)
                 q[kk][j] = (reinterpret_cast<const u32x4 *>(qr + kk * 32)[0][j] & a.score.q_and) ^ a.score.q_xor;
-    }
+    };
+    if constexpr (!TREE)
+        read_row();
+    else if (a.score.ranges)
+        mask = token_mask<TREE>(a, u, len, q_pos0, token, slope);
     // what the wave's rows see, and the workgroup's: without ranges from the first and the last row's positions
     Limits mine, all;
     if (a.score.ranges) {
@@ -285,7 +309,29 @@ __global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
         return m;
     };
     // Cap, bias and masks of the tile at kt, and the running maximum with them (top: the lane's largest score as it came).
-    auto masks = [&](f32x16 (&x)[NB], int kt, float top) __attribute__((always_inline)) {
+    __shared__ __attribute__((aligned(16))) int lds_pos[TREE ? 4 : 1][64];  // positions of a tile's keys where the tree's are among them
+    auto positions = [&](int nb, int g) __attribute__((always_inline)) { return *reinterpret_cast<const i32x4 *>(&lds_pos[TREE ? wave : 0][nb * 32 + 8 * g + 4 * h]); };
+    // A tile with keys of the tree: their positions into LDS, and which of the lane's are on its token's branch (bit i: key kt + 4 h + i).
+    auto branch_of = [&](int kt) __attribute__((always_inline)) {
+        lds_pos[TREE ? wave : 0][lane] = tree_position(a, u, tree_begin, kt + lane);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // (a wave's own LDS accesses stay in order)
+        const int my_token = place_again().token;
+        uint64_t bits = tree_bits(a, u, tree_begin, my_token, kt + 4 * h);
+        if (tree_is_cut(a, u)) {
+            const TreeCut cut(a, u, my_token);
+#pragma unroll 1
+            for (int g = 0; g < 4 * NB; ++g) {
+                const i32x4 pos = positions(0, g);
+                uint64_t left = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    left |= cut.leaves(mask.q_pos, pos[i]) ? 1ull << i : 0ull;
+                bits &= ~(15ull << 8 * g) | left << 8 * g;
+            }
+        }
+        return bits;
+    };
+    auto masks = [&](f32x16 (&x)[NB], int kt, float top, uint64_t branch) __attribute__((always_inline)) {
         const RunMask run(mask, kt + 4 * h);
         const bool masked = kt < mine.full_lo || kt + BN > mine.full_hi;
         if constexpr (MOD == kCapped) {  // -1 / (1 + exp(2 s / cap)): twice the cap times that, and the cap, is cap tanh(s / cap)
@@ -311,21 +357,26 @@ __global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
                         x[nb][i] = fmaf(x[nb][i], f, fmaf(mask.slope2, (float)(nb * 32 + 8 * (i / 4) + i % 4), nearest));
+            } else if (a.score.slopes && in_tree(kt)) {
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const i32x4 pos = positions(nb, g);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            x[nb][g * 4 + i] = biased(x[nb][g * 4 + i] * f, mask, mask.q_pos - pos[i]);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
             } else if (a.score.slopes) {
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int key = nb * 32 + 8 * (i / 4) + i % 4;
-                        const int apart = in_tree(kt) ? tree_apart(a, u, tree_begin, mask.q_pos, kt + 4 * h + key) : run.q - key;
-                        x[nb][i] = biased(x[nb][i] * f, mask, apart);
-                    }
+                    for (int i = 0; i < 16; ++i)
+                        x[nb][i] = biased(x[nb][i] * f, mask, run.q - (nb * 32 + 8 * (i / 4) + i % 4));
             }
         }
-        if (masked) {
-            uint64_t branch = 0;
-            if (in_tree(kt))
-                branch = tree_sees(a, u, tree_begin, token, mask.q_pos, kt + 4 * h, BN);
+        if (masked)
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -333,7 +384,6 @@ __global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
                     const int key = nb * 32 + 8 * (i / 4) + i % 4;
                     x[nb][i] = run.sees(mask, key) || (TREE && (branch >> key & 1u)) ? x[nb][i] : -INFINITY;
                 }
-        }
         if (MOD != kPlain || masked)
             top = top_of(x, 0, 16 * NB, -INFINITY);
         const float mt = wave_xor_max<32>(top) * c;
@@ -372,9 +422,10 @@ __global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
         return true;
     };
     auto add_nonfinite = [&](int kt) __attribute__((always_inline)) {
+        const int my_token = TREE ? place_again().token : 0;
 #pragma unroll 1
         for (int key = kt; key <= min(kt + BN - 1, t_last); ++key) {
-            if (!sees(mask, key) && !(in_tree(kt) && key >= tree_begin && tree_sees(a, u, tree_begin, token, mask.q_pos, key, 1)))
+            if (!sees(mask, key) && !(in_tree(kt) && tree_sees(a, u, tree_begin, my_token, mask.q_pos, key)))
                 continue;
             const char *v = v_base + token_offset(a, table, key);
 #pragma unroll
@@ -391,6 +442,9 @@ __global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
     if (kt < hi) {
         load(kt, 0);
     }
+    if constexpr (TREE)
+        read_row();  // (while the first tile comes)
+    const bool idle = TREE && wave * 32 >= it.n_rows;
     while (kt < hi) {
         all_loads_done();  // the wave's own ...
         __syncthreads();   // ... and everybody's; and everybody has done with the buffers that are loaded next
@@ -400,7 +454,10 @@ __global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
         }
         const bool bad = partly(kt) && clean(v_lds[buf]);
         const char *const kb = k_lds[buf], *const vb = v_lds[buf];
-        if (kt < mine.any_hi && kt + BN > mine.any_lo) {  // (some tiles only other waves' rows see)
+        if (!idle && kt < mine.any_hi && kt + BN > mine.any_lo) {  // (some tiles only other waves' rows see)
+            uint64_t branch = 0;
+            if (in_tree(kt))
+                branch = branch_of(kt);
             f32x16 s[NB];
             // (pieces are read one ahead of their use)
             u32x4 kf[2][NB];
@@ -414,8 +471,12 @@ __global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
                     __builtin_amdgcn_sched_barrier(0);
             }
             vpiece vf[2][CB];
-            read_v(vb, 0, vf[0]);
-            masks(s, kt, top_of(s, 0, 16 * NB, -INFINITY));
+            constexpr bool kLate = TREE && MOD == kGeneral;  // (no registers for it in front of the masks)
+            if constexpr (!kLate)
+                read_v(vb, 0, vf[0]);
+            masks(s, kt, top_of(s, 0, 16 * NB, -INFINITY), branch);
+            if constexpr (kLate)
+                read_v(vb, 0, vf[0]);
             weigh(s, 0, 16 * NB);
 #pragma unroll
             for (int m = 0; m < kSteps; ++m) {
@@ -432,14 +493,15 @@ __global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
         kt = following;
     }
 
+    const Place at_end = place_again();
     const float total = wave_xor_sum<32>(l[0] + l[1]);
     const bool stored = wave * 32 + n < it.n_rows;
     const float inv = total == 0.f ? 0.f : 1.f / total;
     const float lse2 = total == 0.f ? -INFINITY : (mc == -INFINITY ? 0.f : mc) + fast_log2(total) - kShift<DT> + (MOD == kCapped ? a.score.cap_out : 0.f);
-    const float offset = MOD == kGeneral && a.score.slopes ? -a.score.slopes[head] * (float)mask.dist0 : 0.f;
+    const float offset = MOD == kGeneral && a.score.slopes ? -a.score.slopes[at_end.head] * (float)mask.dist0 : 0.f;
     if (!stored)
         return;
-    const int64_t at = (int64_t)(u.tok0 + token) * a.Hq + head;
+    const int64_t at = (int64_t)(u.tok0 + at_end.token) * a.Hq + at_end.head;
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
@@ -459,6 +521,25 @@ __global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
             a.part_lse[(int64_t)it.slot * kManyRows + wave * 32 + n] = float2{lse2, offset};
         else
             a.lse[at] = lse2 * kLn2 + offset;
+    }
+}
+
+template <int DT, int D, bool EXACT, int MOD, bool TREE>
+__global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
+{
+    __shared__ __attribute__((aligned(16))) char k_lds[2][Tiles<DT, D>::kBytes], v_lds[2][Tiles<DT, D>::kBytes];
+    const Tiles<DT, D> lds = {k_lds, v_lds};
+    if constexpr (TREE) {
+        const TreeItem x = scalar_load(reinterpret_cast<const TreeItem *>(a.items), a.first_piece + (int)blockIdx.x);
+        if (x.it.n_rows == 0)
+            return;  // (fills up the launch order)
+        many_item<DT, D, EXACT, MOD, TREE>(a, x.it, x.u, lds);
+    } else {
+        const TokItem it = scalar_load(a.items, blockIdx.x);
+        if (it.n_rows == 0)
+            return;  // (fills up the launch order)
+        const TokUser u = scalar_load(a.users, it.user);
+        many_item<DT, D, EXACT, MOD, TREE>(a, it, u, lds);
     }
 }
 

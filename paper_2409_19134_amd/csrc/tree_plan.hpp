@@ -12,7 +12,7 @@ namespace spd {
 struct PlanUser {
     int32_t token, n, first;  // its first token among all, how many, the position of tokens without a parent
 };
-constexpr int kPlanUsers = 128;
+constexpr int kPlanUsers = 256;
 struct PlanUsers {
     PlanUser it[kPlanUsers];
 };
@@ -61,62 +61,60 @@ __global__ __launch_bounds__(64) void plan_small_kernel(const PlanArgs a, const 
         a.positions[t] = u.first + depth;
 }
 
-// Up to 64 * SPD_MAX_TREE_WORDS tokens: first every jump table, by all threads, then the waves take the words of the sets in turn; depths are summed over them.
-constexpr int kPlanThreads = 512;
+// More tokens, up to `MOST` words of sets in all: every word of every set is a thread's, four or sixteen to a thread; the sets wait in LDS in the order in
+// which they are written.
+constexpr int kPlanThreads = 1024;
+template <int MOST>
 __global__ __launch_bounds__(kPlanThreads) void plan_kernel(const PlanArgs a, const PlanUsers users)
 {
-    constexpr int kMost = 64 * SPD_MAX_TREE_WORDS, kSteps = 10, kWaves = kPlanThreads / 64;
-    static_assert(1 << kSteps >= kMost);
-    __shared__ int16_t jumps[kSteps][kMost];
-    __shared__ uint64_t sets[kWaves][kMost];
-    __shared__ int sizes[kMost];
+    constexpr int kMine = MOST / kPlanThreads;
+    __shared__ uint64_t sets[MOST];
+    __shared__ int16_t jumps[2][64 * SPD_MAX_TREE_WORDS];
     const PlanUser u = users.it[blockIdx.x];
-    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), n = u.n;
-    for (int i = tid; i < n; i += kPlanThreads) {
-        jumps[0][i] = (int16_t)plan_parent(a, u, i);
-        sizes[i] = 0;
+    const int tid = threadIdx.x, W = a.words, n = u.n, n_sets = n * W;  // (n is at most kPlanThreads)
+    int mine = tid < n ? plan_parent(a, u, tid) : -1;
+    if (tid < n)
+        jumps[0][tid] = (int16_t)mine;
+    int token[kMine];
+#pragma unroll
+    for (int m = 0; m < kMine; ++m) {
+        const int e = m * kPlanThreads + tid;
+        token[m] = e / W;
+        const int word = e - token[m] * W;
+        if (e < n_sets)
+            sets[e] = token[m] >> 6 == word ? 1ull << (token[m] & 63) : 0ull;
+        token[m] = e < n_sets ? token[m] : -1;
     }
-    int steps = 0;  // tables that hold a jump
-    for (;;) {
-        bool any = false;
-        __syncthreads();
-        for (int i = tid; i < n; i += kPlanThreads) {
-            const int j = jumps[steps][i];
-            any = any || j >= 0;
-            if (steps + 1 < kSteps)
-                jumps[steps + 1][i] = j >= 0 ? jumps[steps][j] : (int16_t)-1;
+    int now = 0;
+    while (__syncthreads_or(mine >= 0) != 0) {
+        uint64_t other[kMine];
+#pragma unroll
+        for (int m = 0; m < kMine; ++m) {
+            const int e = m * kPlanThreads + tid, j = token[m] >= 0 ? jumps[now][token[m]] : -1;
+            other[m] = j >= 0 ? sets[e - (token[m] - j) * W] : 0ull;
         }
-        if (__syncthreads_or(any) == 0)
-            break;
-        if (++steps == kSteps)
-            break;
+        mine = mine >= 0 ? jumps[now][mine] : -1;
+        if (tid < n)
+            jumps[now ^ 1][tid] = (int16_t)mine;
+#pragma unroll
+        for (int m = 0; m < kMine; ++m)
+            if (other[m])
+                sets[m * kPlanThreads + tid] |= other[m];
+        now ^= 1;
     }
-    for (int w = wave; w < a.words; w += kWaves) {
-        for (int i = lane; i < n; i += 64)
-            sets[wave][i] = i >> 6 == w ? 1ull << (i & 63) : 0ull;
-        // (the wave's own part of LDS: its reads and writes stay in order)
-        for (int k = 0; k < steps; ++k) {
-            __builtin_amdgcn_wave_barrier();
-            for (int i = lane; i < n; i += 64) {
-                const int j = jumps[k][i];
-                if (j >= 0)
-                    sets[wave][i] |= sets[wave][j];
-            }
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        }
-        for (int i = lane; i < n; i += 64) {
-            const uint64_t s = sets[wave][i];
-            a.seen[(int64_t)(u.token + i) * a.words + w] = s;
-            if (s)
-                atomicAdd(&sizes[i], __builtin_popcountll(s));
-        }
-    }
-    __syncthreads();
-    for (int i = tid; i < n; i += kPlanThreads) {
-        a.depth[u.token + i] = sizes[i] - 1;
-        if (a.positions)
-            a.positions[u.token + i] = u.first + sizes[i] - 1;
-    }
+    uint64_t *const out = a.seen + (int64_t)u.token * W;
+#pragma unroll
+    for (int m = 0; m < kMine; ++m)
+        if (token[m] >= 0)
+            out[m * kPlanThreads + tid] = sets[m * kPlanThreads + tid];
+    if (tid >= n)
+        return;
+    int depth = -1;
+    for (int w = 0; w < W; ++w)
+        depth += __builtin_popcountll(sets[tid * W + w]);
+    a.depth[u.token + tid] = depth;
+    if (a.positions)
+        a.positions[u.token + tid] = u.first + depth;
 }
 
 }  // namespace spd
