@@ -644,9 +644,7 @@ class Context:
     def spd_tree_plan(self, parents: torch.Tensor, n_new, first=None, words: Optional[int] = None, tree: Optional[Tree] = None, stream=None) -> Tree:
         """The Tree of drafted tokens from their parents (int32 [T]: a number among the user's own drafted tokens, -1: none), n_new[u] of user u;
         with first (a host sequence: the position of each user's tokens without a parent) its positions too.  tree: one to write into."""
-        counts = np.ascontiguousarray(n_new, dtype=np.int32)
-        assert counts.ndim == 1
-        counts, T = _new_counts(counts, counts.shape[0])
+        counts, T = _new_counts(n_new, len(n_new))
         if tree is None:
             tree = Tree(T, max(1, -(-int(counts.max(initial=0)) // 64)) if words is None else words, device=parents.device)
         assert words is None or tree.struct.n_words == words
@@ -677,8 +675,9 @@ class Context:
         counts, T = _new_counts(n_last, views[0].struct.n_users)
         for t, n in ((keep, T), (n_keep, counts.shape[0])):
             assert t.dtype is torch.int32 and t.is_contiguous() and t.shape == (n,)
+        here = {self.device}
         for v in views:
-            self._here(v)
+            assert v.devices <= here
         self._here(None, keep, n_keep)
         rc = lib.spd_keep_tokens(self.handle, C.byref(shape), _view_array(views), len(views), _address(counts), keep.data_ptr(), n_keep.data_ptr(),
                                  _stream_ptr(stream, self.device))
@@ -691,11 +690,12 @@ class Context:
             return
         assert pairs.dtype is torch.int32 and pairs.is_contiguous() and pairs.dim() == 2 and pairs.shape[1] == 2
         assert n_tokens is None or (n_tokens.dtype is torch.int32 and n_tokens.is_contiguous() and n_tokens.shape == (pairs.shape[0],))
+        here = {self.device}
         for v in views:
-            assert v.struct.block_size
-            self._here(v)
+            assert v.struct.block_size and v.devices <= here
+        n_pages = min([v.n_pages for v in views])
         self._here(None, pairs, n_tokens)
-        rc = lib.spd_copy_pages(self.handle, C.byref(shape), _view_array(views), len(views), min(v.n_pages for v in views), pairs.shape[0],
+        rc = lib.spd_copy_pages(self.handle, C.byref(shape), _view_array(views), len(views), n_pages, pairs.shape[0],
                                 pairs.data_ptr(), None if n_tokens is None else n_tokens.data_ptr(), _stream_ptr(stream, self.device))
         self._check(rc, "spd_copy_pages")
 

@@ -13,17 +13,21 @@ struct KeepUser {
     int32_t user, token;      // its number, and its first entry of the list
     int32_t begin, n;         // the place that entry 0 means, and how many places there are
 };
-constexpr int kKeepUsers = 64;  // (times layers, K and V, heads and slices: a wave's number keeps to 32 bits)
+// Users and layers travel with a launch's arguments, which cost the host by their size: few or many.  (Users times layers, K and V, heads and slices: a
+// stream's number keeps to 32 bits.)
+constexpr int kKeepUsers = 64, kKeepFew = 16;
+template <int N>
 struct KeepUsers {
-    KeepUser it[kKeepUsers];
+    KeepUser it[N];
 };
 struct KeepLayer {
     char *kv[2];              // paged: the pools; else arrays of the users' buffers, on the device
     const int32_t *table;     // paged
 };
-constexpr int kKeepLayers = 32;
+constexpr int kKeepLayers = 32, kKeepFewLayers = 8;
+template <int N>
 struct KeepLayers {
-    KeepLayer it[kKeepLayers];
+    KeepLayer it[N];
 };
 
 struct KeepArgs {
@@ -37,8 +41,8 @@ struct KeepArgs {
 // Tokens kept, in place.  A stream is a slice of the channels of one head of K or V of one user and layer.  WAVES waves have it to themselves and go through
 // the kept tokens in order, some at a time: all of them are read before any is written.  Place i gets what lay at keep[i] >= i: later entries
 // are read at or behind their own places, so never where earlier ones were written, and nothing has to be asked of other workgroups.
-template <int RB, bool PAGED, int WAVES>
-__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void keep_kernel(const KeepArgs a, const KeepUsers users, const KeepLayers layers)
+template <int RB, bool PAGED, int WAVES, int USERS, int LAYERS>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void keep_kernel(const KeepArgs a, const KeepUsers<USERS> users, const KeepLayers<LAYERS> layers)
 {
     constexpr int kLoads = WAVES == 1 ? (RB > 256 ? 4 : 2) : 8;
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
@@ -108,9 +112,10 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void keep_kernel(con
     }
 }
 
-constexpr int kPageLayers = 64;
+constexpr int kPageLayers = 64, kPageFewLayers = 8;
+template <int N>
 struct PageLayers {
-    char *kv[kPageLayers][2];
+    char *kv[N][2];
 };
 struct PageArgs {
     const int32_t *pairs, *n_tokens;     // n_tokens: or nullptr
@@ -122,8 +127,8 @@ struct PageArgs {
 // Pages copied: a workgroup takes so much of a page of K or V in one layer as its threads hold in kPageLoads pieces of sixteen bytes.
 // DENSE: a page's bytes lie end to end, tokens in order (or whole pages in any order).  ONCE: past the caches.
 constexpr int kPageLoads = 1, kPagePieces = 256 * kPageLoads;
-template <int RB, bool DENSE, bool ONCE>
-__global__ __launch_bounds__(256) void copy_pages_kernel(const PageArgs a, const PageLayers layers)
+template <int RB, bool DENSE, bool ONCE, int LAYERS>
+__global__ __launch_bounds__(256) void copy_pages_kernel(const PageArgs a, const PageLayers<LAYERS> layers)
 {
     constexpr int C = RB / 16;
     uint32_t id = a.first + blockIdx.x;

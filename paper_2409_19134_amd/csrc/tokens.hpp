@@ -241,16 +241,16 @@ struct KeyWalk {
 };
 
 // Trees.  Depths are what the caller's memory holds: they are kept to what a tree of so many tokens can have.
-__device__ __forceinline__ int tree_depth(const TokArgs &a, const TokUser &u, int token) { return clampi(a.tree.depth[u.tok0 + token], 0, u.n_tok - 1); }
+__host__ __device__ __forceinline__ int tree_depth(const TokArgs &a, const TokUser &u, int token) { return clampi(a.tree.depth[u.tok0 + token], 0, u.n_tok - 1); }
 // The view's keys in front of the tree: those that order, windows, prefixes and ranges decide about.
 template <bool TREE>
-__device__ __forceinline__ int plain_keys(const TokArgs &a, const TokUser &u, int len)
+__host__ __device__ __forceinline__ int plain_keys(const TokArgs &a, const TokUser &u, int len)
 {
     return TREE && a.tree.inside ? len - u.n_tok : len;
 }
 // A token's masks.  (Inside the view, a tree's token is its own nearest key.)
 template <bool TREE>
-__device__ __forceinline__ RowMask token_mask(const TokArgs &a, const TokUser &u, int len, int q_pos0, int token, float slope)
+__host__ __device__ __forceinline__ RowMask token_mask(const TokArgs &a, const TokUser &u, int len, int q_pos0, int token, float slope)
 {
     RowMask r = row_mask(a.score, u, plain_keys<TREE>(a, u, len), q_pos0 + (TREE ? tree_depth(a, u, token) : token), token, slope);
     if (TREE && a.tree.inside)
@@ -259,13 +259,13 @@ __device__ __forceinline__ RowMask token_mask(const TokArgs &a, const TokUser &u
 }
 // ... of a tile's rows `first` .. `last` without ranges.  A tree's tokens lie at any depth, in any order.
 template <bool TREE>
-__device__ __forceinline__ Limits token_limits(const TokArgs &a, const TokUser &u, int len, int q_pos0, int first, int last)
+__host__ __device__ __forceinline__ Limits token_limits(const TokArgs &a, const TokUser &u, int len, int q_pos0, int first, int last)
 {
     return tile_limits(a.score, u, plain_keys<TREE>(a, u, len), q_pos0 + (TREE ? 0 : first), q_pos0 + (TREE ? u.n_tok - 1 : last));
 }
 // The tree's own keys, which some row sees and not every one.
 template <bool TREE>
-__device__ __forceinline__ void add_tree(Limits &l, const TokArgs &a, const TokUser &u, int len)
+__host__ __device__ __forceinline__ void add_tree(Limits &l, const TokArgs &a, const TokUser &u, int len)
 {
     if (TREE && a.tree.inside) {
         const int base = len - u.n_tok;
@@ -276,7 +276,7 @@ __device__ __forceinline__ void add_tree(Limits &l, const TokArgs &a, const TokU
     }
 }
 // Which of the 64 keys from `key` on are tokens of the tree, which begins at key `base`, that are in a token's set.
-__device__ __forceinline__ uint64_t tree_bits(const TokArgs &a, const TokUser &u, int base, int token, int key)
+__host__ __device__ __forceinline__ uint64_t tree_bits(const TokArgs &a, const TokUser &u, int base, int token, int key)
 {
     const int first = key - base, word = first >> 6, shift = first & 63;
     const uint64_t *const set = a.tree.seen + (int64_t)(u.tok0 + token) * a.tree.words;
@@ -289,15 +289,15 @@ __device__ __forceinline__ uint64_t tree_bits(const TokArgs &a, const TokUser &u
     return left >= 64 ? bits : left > 0 ? bits & ((1ull << left) - 1) : 0ull;
 }
 // The position of a key, which may be one of the tree's (or lie behind them).
-__device__ __forceinline__ int tree_position(const TokArgs &a, const TokUser &u, int base, int key)
+__host__ __device__ __forceinline__ int tree_position(const TokArgs &a, const TokUser &u, int base, int key)
 {
     return key < base ? key : base + tree_depth(a, u, min(key - base, u.n_tok - 1));
 }
 // What windows shorter than the tree may be deep, and documents, leave of a token's set.
-__device__ __forceinline__ bool tree_is_cut(const TokArgs &a, const TokUser &u) { return a.score.ranges || (a.score.window && a.score.window < u.n_tok); }
+__host__ __device__ __forceinline__ bool tree_is_cut(const TokArgs &a, const TokUser &u) { return a.score.ranges || (a.score.window && a.score.window < u.n_tok); }
 struct TreeCut {
     int lo = 0, hi = 0x7fffffff, window = 0x7fffffff;
-    __device__ __forceinline__ TreeCut(const TokArgs &a, const TokUser &u, int token)
+    __host__ __device__ __forceinline__ TreeCut(const TokArgs &a, const TokUser &u, int token)
     {
         if (a.score.ranges) {
             const int2 v = reinterpret_cast<const int2 *>(a.score.ranges)[u.tok0 + token];
@@ -307,10 +307,10 @@ struct TreeCut {
         if (a.score.window)
             window = a.score.window;
     }
-    __device__ __forceinline__ bool leaves(int q_pos, int pos) const { return pos >= lo && pos < hi && abs(q_pos - pos) < window; }
+    __host__ __device__ __forceinline__ bool leaves(int q_pos, int pos) const { return pos >= lo && pos < hi && abs(q_pos - pos) < window; }
 };
 // All of it for one key.
-__device__ __forceinline__ bool tree_sees(const TokArgs &a, const TokUser &u, int base, int token, int q_pos, int key)
+__host__ __device__ __forceinline__ bool tree_sees(const TokArgs &a, const TokUser &u, int base, int token, int q_pos, int key)
 {
     return key >= base && (tree_bits(a, u, base, token, key) & 1u) && TreeCut(a, u, token).leaves(q_pos, tree_position(a, u, base, key));
 }
@@ -444,10 +444,13 @@ __device__ __forceinline__ void store4(const TokArgs &a, int64_t at, f32x4 v)
 // Launches (host): `rows` is the row capacity of the few kernel's tiles, 16 or 32.
 __attribute__((visibility("hidden"))) void launch_tokens_few(int dtype, int head_dim, bool paged, int rows, bool modified, bool tree,
                                                              int64_t n_items, const TokArgs &a, hipStream_t stream);
-__attribute__((visibility("hidden"))) void launch_tokens_many(int dtype, int head_dim, bool modified, bool tree, int64_t n_items,
+__attribute__((visibility("hidden"))) void launch_tokens_many(int dtype, int head_dim, bool modified, bool tree, bool half, int64_t n_items,
                                                               const TokArgs &a, hipStream_t stream);
 constexpr int kManyRows = 128;  // rows of a tile of the many kernel
-__host__ __device__ constexpr int many_keys(int dtype) { return dtype == SPD_F32 ? 32 : 64; }  // keys of its steps
+constexpr int kHalfRows = 64;   // ... of its form (of trees) in which two waves share 32 rows
+__host__ __device__ constexpr int many_keys(int dtype, bool half = false) { return dtype == SPD_F32 && !half ? 32 : 64; }  // keys of its steps
+// Where there is such a form (fp32 heads of 128 have no room for steps of 64 keys in LDS).
+__host__ __device__ constexpr bool has_half(int dtype, int head_dim) { return dtype != SPD_F32 || head_dim == 64; }
 // Workgroups of the few kernel's tree form that fit on a compute unit, by its rows.
 __host__ __device__ constexpr int tree_resident(int dtype, int head_dim, int rows)
 {

@@ -90,7 +90,7 @@ struct TokEntry {
     size_t off_items[host::kTokKernels] = {}, off_joins[host::kTokKernels] = {};
     int64_t n_items[host::kTokKernels] = {}, n_joins[host::kTokKernels] = {}, slots[host::kTokKernels] = {};
     int join_rows[host::kTokKernels] = {}, join_chunks[host::kTokKernels] = {};
-    bool growable = false, following = false;  // as in TokTables
+    bool growable = false, following = false, half = false;  // as in TokTables
     // append
     int64_t n_append = 0;
 };
@@ -439,6 +439,7 @@ int find_or_build(ContextBase *ctx, TokensState *t, const spd_shape *s, const sp
     }
     e->growable = T.growable;
     e->following = T.following;
+    e->half = T.half;
     e->key = t->key;
     e->hash = hash;
     e->lens = t->lens;
@@ -514,10 +515,11 @@ int attend(ContextBase *ctx, const spd_shape *s, const void *q, int64_t q_stride
     rc = find_or_build(ctx, t, s, v, c, tree != nullptr, stream, in_graph, &e, &grow_len, &grow_q);
     if (rc != SPD_OK)
         return rc;
+    auto tile_of = [e](int k) { return e->half && k == (int)TokKernel::kMany ? kHalfRows : tile_rows((TokKernel)k); };
     size_t rows[kTokKernels], part_rows = 0;
     for (int k = 0; k < kTokKernels; ++k) {
         rows[k] = part_rows;
-        part_rows += (size_t)e->slots[k] * (size_t)tile_rows((TokKernel)k);
+        part_rows += (size_t)e->slots[k] * (size_t)tile_of(k);
     }
     rc = ensure_parts(ctx, t, part_rows * ((size_t)s->head_dim * sizeof(float) + sizeof(float2)), in_graph);
     if (rc != SPD_OK)
@@ -572,7 +574,7 @@ int attend(ContextBase *ctx, const spd_shape *s, const void *q, int64_t q_stride
     for (int k = 0; k < kTokKernels; ++k) {
         if (e->n_items[k] == 0)
             continue;
-        const int cap = tile_rows((TokKernel)k);
+        const int cap = tile_of(k);
         const TokItem *const items = reinterpret_cast<const TokItem *>(e->dev + e->off_items[k]);
         a.part_o = t->part + rows[k] * (size_t)s->head_dim;
         a.part_lse = part_lse + rows[k];
@@ -580,7 +582,7 @@ int attend(ContextBase *ctx, const spd_shape *s, const void *q, int64_t q_stride
             a.items = tree ? items : items + first;
             a.first_piece = (int32_t)first;
             if (k == (int)TokKernel::kMany)
-                launch_tokens_many(s->dtype, s->head_dim, modified, tree != nullptr, n, a, stream);
+                launch_tokens_many(s->dtype, s->head_dim, modified, tree != nullptr, e->half, n, a, stream);
             else
                 launch_tokens_few(s->dtype, s->head_dim, paged, cap, modified, tree != nullptr, n, a, stream);
         });
@@ -777,6 +779,16 @@ int append(ContextBase *ctx, const spd_shape *s, const spd_kv_view *v, const int
     return SPD_OK;
 }
 
+// f gets the smaller of two sizes that holds n, as an integral constant.
+template <int FEW, int MANY, class F>
+void by_size(int n, F &&f)
+{
+    if (n <= FEW)
+        f(std::integral_constant<int, FEW>());
+    else
+        f(std::integral_constant<int, MANY>());
+}
+
 int tree_plan(ContextBase *ctx, int32_t n_users, const int32_t *n_new, const int32_t *parents, const int32_t *first, int32_t words, uint64_t *seen,
               int32_t *depth, int32_t *positions, hipStream_t stream)
 {
@@ -792,16 +804,18 @@ int tree_plan(ContextBase *ctx, int32_t n_users, const int32_t *n_new, const int
     const OnDevice on(ctx->device);
     SPD_TRY(ctx, on.error);
     // A launch's users travel with its arguments: those that have tokens, so many at a time.
-    PlanUsers users;
+    PlanUsers<kPlanUsers> users;
     int32_t token = 0, n = 0, most = 0;
     auto launch = [&]() -> int {
         if (n == 0)
             return SPD_OK;
-        if (most <= 64)
-            hipLaunchKernelGGL(plan_small_kernel, dim3((unsigned)n), dim3(64), 0, stream, a, users);
-        else
-            hipLaunchKernelGGL(most * words <= 4096 ? plan_kernel<4096> : plan_kernel<64 * SPD_MAX_TREE_WORDS * SPD_MAX_TREE_WORDS>, dim3((unsigned)n),
-                               dim3(kPlanThreads), 0, stream, a, users);
+        by_size<kPlanFew, kPlanUsers>(n, [&](auto size) {
+            constexpr int kAll = 64 * SPD_MAX_TREE_WORDS * SPD_MAX_TREE_WORDS;
+            PlanUsers<size()> some;
+            std::memcpy(some.it, users.it, (size_t)n * sizeof(PlanUser));
+            const auto kernel = most <= 64 ? plan_small_kernel<size()> : most * words <= 4096 ? plan_kernel<4096, size()> : plan_kernel<kAll, size()>;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)n), dim3(most <= 64 ? 64 : kPlanThreads), 0, stream, a, some);
+        });
         n = most = 0;
         SPD_TRY(ctx, hipGetLastError());
         return SPD_OK;
@@ -894,8 +908,8 @@ int keep_tokens(ContextBase *ctx, const spd_shape *s, const spd_kv_view *views, 
     const int row_bytes = s->head_dim * es;
     const int32_t longest = *std::max_element(n_last, n_last + U);
     const int waves = longest <= 64 ? 1 : longest <= 512 ? 4 : 16;
-    KeepUsers users;
-    KeepLayers layers;
+    KeepUsers<kKeepUsers> users;
+    KeepLayers<kKeepLayers> layers;
     int failed = SPD_OK;
     auto launch = [&](int n_users, int n_layers) {
         const int64_t streams = (int64_t)n_users * n_layers * 2 * s->n_kv_heads;
@@ -905,13 +919,24 @@ int keep_tokens(ContextBase *ctx, const spd_shape *s, const spd_kv_view *views, 
         a.n_streams = (uint32_t)streams;
         a.n_layers = n_layers;
         const int threads = std::max(256, 64 * waves), per_group = threads / 64 / waves;
-        with_row_bytes(row_bytes, [&](auto rb) {
-            auto kernel = waves == 1 ? (paged ? keep_kernel<rb(), true, 1> : keep_kernel<rb(), false, 1>)
-                          : waves == 4 ? (paged ? keep_kernel<rb(), true, 4> : keep_kernel<rb(), false, 4>)
-                                       : (paged ? keep_kernel<rb(), true, 16> : keep_kernel<rb(), false, 16>);
+        auto send = [&](auto kernel, const auto &some, const auto &of_layers) {
             in_parts(((waves == 1 ? streams : (streams + 7) / 8 * 8) * a.slices + per_group - 1) / per_group, [&](int64_t first, unsigned n) {
                 a.first = (uint32_t)(first * per_group);
-                hipLaunchKernelGGL(kernel, dim3(n), dim3((unsigned)threads), 0, stream, a, users, layers);
+                hipLaunchKernelGGL(kernel, dim3(n), dim3((unsigned)threads), 0, stream, a, some, of_layers);
+            });
+        };
+        with_row_bytes(row_bytes, [&](auto rb) {
+            by_size<kKeepFew, kKeepUsers>(n_users, [&](auto nu) {
+                by_size<kKeepFewLayers, kKeepLayers>(n_layers, [&](auto nl) {
+                    KeepUsers<nu()> some;
+                    KeepLayers<nl()> of_layers;
+                    std::memcpy(some.it, users.it, (size_t)n_users * sizeof(KeepUser));
+                    std::memcpy(of_layers.it, layers.it, (size_t)n_layers * sizeof(KeepLayer));
+                    auto kernel = waves == 1   ? (paged ? keep_kernel<rb(), true, 1, nu(), nl()> : keep_kernel<rb(), false, 1, nu(), nl()>)
+                                  : waves == 4 ? (paged ? keep_kernel<rb(), true, 4, nu(), nl()> : keep_kernel<rb(), false, 4, nu(), nl()>)
+                                               : (paged ? keep_kernel<rb(), true, 16, nu(), nl()> : keep_kernel<rb(), false, 16, nu(), nl()>);
+                    send(kernel, some, of_layers);
+                });
             });
         });
         const hipError_t e = hipGetLastError();
@@ -980,7 +1005,7 @@ int copy_pages(ContextBase *ctx, const spd_shape *s, const spd_kv_view *views, i
     const int64_t d = s->head_dim, H = s->n_kv_heads;
     const bool dense = (v.head_stride == d && v.token_stride == H * d) || (!n_tokens && v.token_stride == d && v.head_stride == v.block_size * d);
     const bool once = (int64_t)n_pairs * n_views * 2 * v.block_size * H * row_bytes >= kOnceBytes;
-    PageLayers layers;
+    PageLayers<kPageLayers> layers;
     for (int i = 0; i < n_views; i += kPageLayers) {
         const int n_layers = std::min(n_views - i, kPageLayers);
         for (int j = 0; j < n_layers; ++j) {
@@ -990,16 +1015,20 @@ int copy_pages(ContextBase *ctx, const spd_shape *s, const spd_kv_view *views, i
         a.n_layers = n_layers;
         const int64_t groups = (int64_t)n_layers * 2 * a.parts, most = std::max<int64_t>(1, kMostGroups / groups);  // of a pair; pairs of a launch
         with_row_bytes(row_bytes, [&](auto rb) {
-            auto kernel = dense ? (once ? copy_pages_kernel<rb(), true, true> : copy_pages_kernel<rb(), true, false>)
-                                : (once ? copy_pages_kernel<rb(), false, true> : copy_pages_kernel<rb(), false, false>);
-            for (int64_t p = 0; p < n_pairs; p += most) {
-                a.pairs = pairs + 2 * p;
-                a.n_tokens = n_tokens ? n_tokens + p : nullptr;
-                in_parts(groups * std::min(most, n_pairs - p), [&](int64_t first, unsigned n) {
-                    a.first = (uint32_t)first;
-                    hipLaunchKernelGGL(kernel, dim3(n), dim3(256), 0, stream, a, layers);
-                });
-            }
+            by_size<kPageFewLayers, kPageLayers>(n_layers, [&](auto nl) {
+                PageLayers<nl()> some;
+                std::memcpy(some.kv, layers.kv, (size_t)n_layers * sizeof layers.kv[0]);
+                auto kernel = dense ? (once ? copy_pages_kernel<rb(), true, true, nl()> : copy_pages_kernel<rb(), true, false, nl()>)
+                                    : (once ? copy_pages_kernel<rb(), false, true, nl()> : copy_pages_kernel<rb(), false, false, nl()>);
+                for (int64_t p = 0; p < n_pairs; p += most) {
+                    a.pairs = pairs + 2 * p;
+                    a.n_tokens = n_tokens ? n_tokens + p : nullptr;
+                    in_parts(groups * std::min(most, n_pairs - p), [&](int64_t first, unsigned n) {
+                        a.first = (uint32_t)first;
+                        hipLaunchKernelGGL(kernel, dim3(n), dim3(256), 0, stream, a, some);
+                    });
+                }
+            });
         });
         SPD_TRY(ctx, hipGetLastError());
     }

@@ -78,24 +78,41 @@ constexpr float kRaise = 8.f;   // log2 of what a row's largest P may be
 template <int DT>
 constexpr float kShift = DT == SPD_F16 ? 7.f : 0.f;
 
-template <int DT, int D>
+// The kernel's forms.  kTree: for the tokens of a tree.  kTreeHalf: the same for up to 64 rows: two waves share 32 rows, each takes half of every tile's keys, and
+// their sums are joined at the end.  (In the other form two of four waves, and with them two of a unit's four SIMDs, would have no rows.)
+enum { kChain = 0, kTree = 1, kTreeHalf = 2 };
+
+template <int DT, int D, int FORM>
 struct Tiles {
-    static constexpr int kBytes = many_keys(DT) * D * (DT == SPD_F32 ? 4 : 2);
+    static constexpr int kBytes = many_keys(DT, FORM == kTreeHalf) * D * (DT == SPD_F32 ? 4 : 2);
     char (*k)[kBytes], (*v)[kBytes];  // two buffers of each, in LDS
 };
 
-// One item: a tile's rows over a stretch of keys.
-template <int DT, int D, bool EXACT, int MOD, bool TREE>
-__device__ __forceinline__ void many_item(const TokArgs &a, const TokItem &it, const TokUser &u, const Tiles<DT, D> lds)
+// The kernel's arguments, in the tree form read anew where a tile's end or the tree's own keys need them: the loop over the keys has no scalar registers for them.
+template <bool TREE>
+__device__ __forceinline__ const TokArgs &arguments(const TokArgs &a)
 {
-    constexpr bool kF32 = DT == SPD_F32;
-    constexpr int kBytes = kF32 ? 4 : 2, RB = D * kBytes, BN = many_keys(DT), NB = BN / 32, C = RB / 16, KK = RB / 32, CB = D / 32;
+    if constexpr (!TREE)
+        return a;
+    const __attribute__((address_space(4))) char *p = (const __attribute__((address_space(4))) char *)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const TokArgs *)(const __attribute__((address_space(4))) TokArgs *)p;
+}
+
+// One item: a tile's rows over a stretch of keys.
+template <int DT, int D, bool EXACT, int MOD, int FORM>
+__device__ __forceinline__ void many_item(const TokArgs &a, const TokItem &it, const TokUser &u, const Tiles<DT, D, FORM> lds)
+{
+    constexpr bool kF32 = DT == SPD_F32, TREE = FORM != kChain, HALF = FORM == kTreeHalf;
+    constexpr int kRows = HALF ? kHalfRows : kManyRows;
+    constexpr int kBytes = kF32 ? 4 : 2, RB = D * kBytes, BN = many_keys(DT, HALF), NB = BN / 32 / (HALF ? 2 : 1), C = RB / 16, KK = RB / 32, CB = D / 32;
     constexpr int kPieces = BN * C / 256;
     constexpr int kTerms = EXACT ? Block<DT>::kTerms : 1;
     auto &k_lds = lds.k;
     auto &v_lds = lds.v;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int n = lane & 31, h = lane >> 5;
+    const int rows_of = (HALF ? wave & 1 : wave) * 32, keys_of = HALF ? (wave >> 1) * (BN / 2) : 0;  // the wave's rows of the tile, and keys of every step
     const int len = u.len + a.grow_len, q_pos0 = u.q_pos + a.grow_q;
     const int k_end = it.k_end + (it.to_len ? a.grow_len : 0);
 
@@ -105,7 +122,7 @@ __device__ __forceinline__ void many_item(const TokArgs &a, const TokItem &it, c
         int token, head;
     };
     auto place = [&](int lane_) __attribute__((always_inline)) {
-        const int my_row = min(it.row0 + wave * 32 + (lane_ & 31), it.row0 + it.n_rows - 1), token_ = my_row / a.G;
+        const int my_row = min(it.row0 + rows_of + (lane_ & 31), it.row0 + it.n_rows - 1), token_ = my_row / a.G;
         return Place{token_, it.kv_head * a.G + (my_row - token_ * a.G)};
     };
     const Place mine_ = place(lane);
@@ -151,8 +168,8 @@ __device__ __forceinline__ void many_item(const TokArgs &a, const TokItem &it, c
         all = all.uniform_of();
     } else {
         auto token_of = [&](int row) { return min(it.row0 + row, it.row0 + it.n_rows - 1) / a.G; };
-        mine = token_limits<TREE>(a, u, len, q_pos0, token_of(wave * 32), token_of(wave * 32 + 31));
-        all = token_limits<TREE>(a, u, len, q_pos0, token_of(0), token_of(kManyRows - 1));
+        mine = token_limits<TREE>(a, u, len, q_pos0, token_of(rows_of), token_of(rows_of + 31));
+        all = token_limits<TREE>(a, u, len, q_pos0, token_of(0), token_of(kRows - 1));
     }
     add_tree<TREE>(mine, a, u, len);
     add_tree<TREE>(all, a, u, len);
@@ -219,8 +236,8 @@ __device__ __forceinline__ void many_item(const TokArgs &a, const TokItem &it, c
     auto partly = [&](int kt) { return kt < all.full_lo || kt + BN > all.full_hi; };
     const float c = MOD == kPlain ? a.score.c : MOD == kCapped ? 2.f * a.score.cap_out : 1.f, steep = 2.f * kLog2e * a.score.cap_in;
     // lane parts of the LDS places: K row n, piece 2 kk + h; V (16-bit) keys 4 h + i / 4 of sixteen channels' pieces
-    const int k_lane_ = n * RB + (h ^ swap(n)) * 16;
-    const int vi = lane & 15, v_row = 4 * h + vi / 4, v_piece = ((lane >> 4) & 1) * 2 + ((vi & 3) >> 1);
+    const int k_lane_ = (keys_of + n) * RB + (h ^ swap(n)) * 16;
+    const int vi = lane & 15, v_row = keys_of + 4 * h + vi / 4, v_piece = ((lane >> 4) & 1) * 2 + ((vi & 3) >> 1);
     const int v_lane[2] = {v_row * RB + (v_piece ^ swap(v_row)) * 16 + (vi & 1) * 8, (v_row + 8) * RB + (v_piece ^ swap(v_row + 8)) * 16 + (vi & 1) * 8};
 
     // Pieces of the two products.  K: the rows' pieces kk of 32 keys each; V (16-bit): sixteen keys' V^T of 32 channels, by two transposed reads; V
@@ -253,7 +270,7 @@ __device__ __forceinline__ void many_item(const TokArgs &a, const TokItem &it, c
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
             if constexpr (kF32) {
-                int key = 8 * (m / 4) + 4 * h + m % 4;
+                int key = keys_of + 8 * (m / 4) + 4 * h + m % 4;
                 asm volatile("" : "+v"(key));
                 f[cb] = *(lds_u32 *)(vp + (key * RB + ((cb * 8 + n / 4) ^ swap(key)) * 16 + n % 4 * 4));
             } else {
@@ -311,14 +328,15 @@ __device__ __forceinline__ void many_item(const TokArgs &a, const TokItem &it, c
     // Cap, bias and masks of the tile at kt, and the running maximum with them (top: the lane's largest score as it came).
     __shared__ __attribute__((aligned(16))) int lds_pos[TREE ? 4 : 1][64];  // positions of a tile's keys where the tree's are among them
     auto positions = [&](int nb, int g) __attribute__((always_inline)) { return *reinterpret_cast<const i32x4 *>(&lds_pos[TREE ? wave : 0][nb * 32 + 8 * g + 4 * h]); };
-    // A tile with keys of the tree: their positions into LDS, and which of the lane's are on its token's branch (bit i: key kt + 4 h + i).
+    // A tile with keys of the tree: their positions into LDS, and which of the lane's are on its token's branch (bit i: key kt + keys_of + 4 h + i).
     auto branch_of = [&](int kt) __attribute__((always_inline)) {
-        lds_pos[TREE ? wave : 0][lane] = tree_position(a, u, tree_begin, kt + lane);
+        const TokArgs &b = arguments<TREE>(a);
+        lds_pos[TREE ? wave : 0][lane] = tree_position(b, u, tree_begin, kt + keys_of + lane);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // (a wave's own LDS accesses stay in order)
         const int my_token = place_again().token;
-        uint64_t bits = tree_bits(a, u, tree_begin, my_token, kt + 4 * h);
-        if (tree_is_cut(a, u)) {
-            const TreeCut cut(a, u, my_token);
+        uint64_t bits = tree_bits(b, u, tree_begin, my_token, kt + keys_of + 4 * h);
+        if (tree_is_cut(b, u)) {
+            const TreeCut cut(b, u, my_token);
 #pragma unroll 1
             for (int g = 0; g < 4 * NB; ++g) {
                 const i32x4 pos = positions(0, g);
@@ -332,8 +350,9 @@ __device__ __forceinline__ void many_item(const TokArgs &a, const TokItem &it, c
         return bits;
     };
     auto masks = [&](f32x16 (&x)[NB], int kt, float top, uint64_t branch) __attribute__((always_inline)) {
-        const RunMask run(mask, kt + 4 * h);
-        const bool masked = kt < mine.full_lo || kt + BN > mine.full_hi;
+        const int first = kt + keys_of;
+        const RunMask run(mask, first + 4 * h);
+        const bool masked = first < mine.full_lo || first + 32 * NB > mine.full_hi;
         if constexpr (MOD == kCapped) {  // -1 / (1 + exp(2 s / cap)): twice the cap times that, and the cap, is cap tanh(s / cap)
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
@@ -342,7 +361,7 @@ __device__ __forceinline__ void many_item(const TokArgs &a, const TokItem &it, c
                     x[nb][i] = fast_rcp(-1.f - fast_exp2(x[nb][i] * steep));
         } else if constexpr (MOD == kGeneral) {
             // Before all of the wave's queries a key's distance grows by one from key to key: the bias is a line, one fma per score.
-            const bool before = a.score.slopes && __builtin_amdgcn_ballot_w64(run.q < BN - 1) == 0 && !in_tree(kt);
+            const bool before = a.score.slopes && __builtin_amdgcn_ballot_w64(run.q < 32 * NB - 1) == 0 && !in_tree(kt);
             const float nearest = mask.slope2 * (float)(mask.dist0 - run.q);
             const float f = a.score.cap_out != 0.f ? 1.f : a.score.c;
             if (a.score.cap_out != 0.f)
@@ -422,12 +441,13 @@ __device__ __forceinline__ void many_item(const TokArgs &a, const TokItem &it, c
         return true;
     };
     auto add_nonfinite = [&](int kt) __attribute__((always_inline)) {
+        const TokArgs &b = arguments<TREE>(a);
         const int my_token = TREE ? place_again().token : 0;
 #pragma unroll 1
-        for (int key = kt; key <= min(kt + BN - 1, t_last); ++key) {
-            if (!sees(mask, key) && !(in_tree(kt) && tree_sees(a, u, tree_begin, my_token, mask.q_pos, key)))
+        for (int key = kt + keys_of; key <= min(kt + keys_of + 32 * NB - 1, t_last); ++key) {
+            if (!sees(mask, key) && !(in_tree(kt) && tree_sees(b, u, tree_begin, my_token, mask.q_pos, key)))
                 continue;
-            const char *v = v_base + token_offset(a, table, key);
+            const char *v = v_base + token_offset(b, table, key);
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb) {
 #pragma unroll
@@ -444,7 +464,7 @@ __device__ __forceinline__ void many_item(const TokArgs &a, const TokItem &it, c
     }
     if constexpr (TREE)
         read_row();  // (while the first tile comes)
-    const bool idle = TREE && wave * 32 >= it.n_rows;
+    const bool idle = TREE && rows_of >= it.n_rows;
     while (kt < hi) {
         all_loads_done();  // the wave's own ...
         __syncthreads();   // ... and everybody's; and everybody has done with the buffers that are loaded next
@@ -454,7 +474,7 @@ __device__ __forceinline__ void many_item(const TokArgs &a, const TokItem &it, c
         }
         const bool bad = partly(kt) && clean(v_lds[buf]);
         const char *const kb = k_lds[buf], *const vb = v_lds[buf];
-        if (!idle && kt < mine.any_hi && kt + BN > mine.any_lo) {  // (some tiles only other waves' rows see)
+        if (!idle && kt + keys_of < mine.any_hi && kt + keys_of + 32 * NB > mine.any_lo) {  // (some tiles only other waves' rows see)
             uint64_t branch = 0;
             if (in_tree(kt))
                 branch = branch_of(kt);
@@ -494,14 +514,46 @@ __device__ __forceinline__ void many_item(const TokArgs &a, const TokItem &it, c
     }
 
     const Place at_end = place_again();
-    const float total = wave_xor_sum<32>(l[0] + l[1]);
-    const bool stored = wave * 32 + n < it.n_rows;
+    float total = wave_xor_sum<32>(l[0] + l[1]);
+    if constexpr (HALF) {  // the second halves' sums through LDS
+        static_assert(CB * 4 * 64 * 16 <= Tiles<DT, D, FORM>::kBytes);
+        __shared__ float lds_ml[2][2][64];
+        __syncthreads();  // (everybody has done with the tiles)
+        f32x4 *const part = reinterpret_cast<f32x4 *>(k_lds[wave & 1]);
+        if (wave >= 2) {
+            lds_ml[0][wave & 1][lane] = mc;
+            lds_ml[1][wave & 1][lane] = total;
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    part[(cb * 4 + g) * 64 + lane] = f32x4{acc[cb][g * 4], acc[cb][g * 4 + 1], acc[cb][g * 4 + 2], acc[cb][g * 4 + 3]};
+        }
+        __syncthreads();
+        if (wave >= 2)
+            return;
+        const float other = lds_ml[0][wave][lane], m = fmaxf(mc, other);
+        const float f0 = mc == -INFINITY ? 0.f : fast_exp2(mc - m), f1 = other == -INFINITY ? 0.f : fast_exp2(other - m);
+        mc = m;
+        total = total * f0 + lds_ml[1][wave][lane] * f1;
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const f32x4 o = part[(cb * 4 + g) * 64 + lane];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    acc[cb][g * 4 + i] = acc[cb][g * 4 + i] * f0 + o[i] * f1;
+            }
+    }
+    const bool stored = rows_of + n < it.n_rows;
     const float inv = total == 0.f ? 0.f : 1.f / total;
     const float lse2 = total == 0.f ? -INFINITY : (mc == -INFINITY ? 0.f : mc) + fast_log2(total) - kShift<DT> + (MOD == kCapped ? a.score.cap_out : 0.f);
-    const float offset = MOD == kGeneral && a.score.slopes ? -a.score.slopes[at_end.head] * (float)mask.dist0 : 0.f;
+    const TokArgs &b = arguments<TREE>(a);
+    const float offset = MOD == kGeneral && b.score.slopes ? -b.score.slopes[at_end.head] * (float)mask.dist0 : 0.f;
     if (!stored)
         return;
-    const int64_t at = (int64_t)(u.tok0 + at_end.token) * a.Hq + at_end.head;
+    const int64_t at = (int64_t)(u.tok0 + at_end.token) * b.Hq + at_end.head;
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
@@ -512,80 +564,83 @@ __device__ __forceinline__ void many_item(const TokArgs &a, const TokItem &it, c
                 o[i] = total == 0.f ? 0.f : acc[cb][g * 4 + i] * inv;
             const int ch = cb * 32 + 8 * g + 4 * h;
             if (it.slot >= 0)
-                *reinterpret_cast<f32x4 *>(a.part_o + ((int64_t)it.slot * kManyRows + wave * 32 + n) * D + ch) = o;
+                *reinterpret_cast<f32x4 *>(b.part_o + ((int64_t)it.slot * kRows + rows_of + n) * D + ch) = o;
             else
-                store4<DT>(a, at * D + ch, o);
+                store4<DT>(b, at * D + ch, o);
         }
     if (h == 0) {
         if (it.slot >= 0)
-            a.part_lse[(int64_t)it.slot * kManyRows + wave * 32 + n] = float2{lse2, offset};
+            b.part_lse[(int64_t)it.slot * kRows + rows_of + n] = float2{lse2, offset};
         else
-            a.lse[at] = lse2 * kLn2 + offset;
+            b.lse[at] = lse2 * kLn2 + offset;
     }
 }
 
-template <int DT, int D, bool EXACT, int MOD, bool TREE>
+template <int DT, int D, bool EXACT, int MOD, int FORM>
 __global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
 {
-    __shared__ __attribute__((aligned(16))) char k_lds[2][Tiles<DT, D>::kBytes], v_lds[2][Tiles<DT, D>::kBytes];
-    const Tiles<DT, D> lds = {k_lds, v_lds};
-    if constexpr (TREE) {
+    __shared__ __attribute__((aligned(16))) char k_lds[2][Tiles<DT, D, FORM>::kBytes], v_lds[2][Tiles<DT, D, FORM>::kBytes];
+    const Tiles<DT, D, FORM> lds = {k_lds, v_lds};
+    if constexpr (FORM != kChain) {
         const TreeItem x = scalar_load(reinterpret_cast<const TreeItem *>(a.items), a.first_piece + (int)blockIdx.x);
         if (x.it.n_rows == 0)
             return;  // (fills up the launch order)
-        many_item<DT, D, EXACT, MOD, TREE>(a, x.it, x.u, lds);
+        many_item<DT, D, EXACT, MOD, FORM>(a, x.it, x.u, lds);
     } else {
         const TokItem it = scalar_load(a.items, blockIdx.x);
         if (it.n_rows == 0)
             return;  // (fills up the launch order)
         const TokUser u = scalar_load(a.users, it.user);
-        many_item<DT, D, EXACT, MOD, TREE>(a, it, u, lds);
+        many_item<DT, D, EXACT, MOD, FORM>(a, it, u, lds);
     }
 }
 
-template <int DT, int D, bool EXACT, bool TREE>
+template <int DT, int D, bool EXACT, int FORM>
 void launch(bool modified, int64_t n_items, const TokArgs &a, hipStream_t stream)
 {
     const dim3 grid((unsigned)n_items), block(256);
     if (!modified)
-        hipLaunchKernelGGL((tokens_many_kernel<DT, D, EXACT, kPlain, TREE>), grid, block, 0, stream, a);
+        hipLaunchKernelGGL((tokens_many_kernel<DT, D, EXACT, kPlain, FORM>), grid, block, 0, stream, a);
     else if (!EXACT && !a.score.slopes && a.score.cap_out <= kCappedMost)
-        hipLaunchKernelGGL((tokens_many_kernel<DT, D, EXACT, EXACT ? kGeneral : kCapped, TREE>), grid, block, 0, stream, a);
+        hipLaunchKernelGGL((tokens_many_kernel<DT, D, EXACT, EXACT ? kGeneral : kCapped, FORM>), grid, block, 0, stream, a);
     else
-        hipLaunchKernelGGL((tokens_many_kernel<DT, D, EXACT, kGeneral, TREE>), grid, block, 0, stream, a);
+        hipLaunchKernelGGL((tokens_many_kernel<DT, D, EXACT, kGeneral, FORM>), grid, block, 0, stream, a);
 }
-template <int DT, int D, bool TREE>
+template <int DT, int D, int FORM>
 void launch(bool modified, int64_t n_items, const TokArgs &a, hipStream_t stream)
 {
     if (DT == SPD_F32 || a.out_f32)
-        launch<DT, D, true, TREE>(modified, n_items, a, stream);
+        launch<DT, D, true, FORM>(modified, n_items, a, stream);
     else if constexpr (DT != SPD_F32)
-        launch<DT, D, false, TREE>(modified, n_items, a, stream);
+        launch<DT, D, false, FORM>(modified, n_items, a, stream);
 }
 template <int DT, int D>
-void launch(bool modified, bool tree, int64_t n_items, const TokArgs &a, hipStream_t stream)
+void launch(bool modified, bool tree, bool half, int64_t n_items, const TokArgs &a, hipStream_t stream)
 {
-    tree ? launch<DT, D, true>(modified, n_items, a, stream) : launch<DT, D, false>(modified, n_items, a, stream);
+    if constexpr (has_half(DT, D))
+        if (half)
+            return launch<DT, D, kTreeHalf>(modified, n_items, a, stream);
+    tree ? launch<DT, D, kTree>(modified, n_items, a, stream) : launch<DT, D, kChain>(modified, n_items, a, stream);
 }
 template <int DT>
-void launch(int head_dim, bool modified, bool tree, int64_t n_items, const TokArgs &a, hipStream_t stream)
+void launch(int head_dim, bool modified, bool tree, bool half, int64_t n_items, const TokArgs &a, hipStream_t stream)
 {
     if (head_dim == 64)
-        launch<DT, 64>(modified, tree, n_items, a, stream);
+        launch<DT, 64>(modified, tree, half, n_items, a, stream);
     else
-        launch<DT, 128>(modified, tree, n_items, a, stream);
+        launch<DT, 128>(modified, tree, half, n_items, a, stream);
 }
 
 }  // namespace
 
-void launch_tokens_many(int dtype, int head_dim, bool modified, bool tree, int64_t n_items, const TokArgs &a, hipStream_t stream)
+void launch_tokens_many(int dtype, int head_dim, bool modified, bool tree, bool half, int64_t n_items, const TokArgs &a, hipStream_t stream)
 {
     if (dtype == SPD_F32)
-        launch<SPD_F32>(head_dim, modified, tree, n_items, a, stream);
+        launch<SPD_F32>(head_dim, modified, tree, half, n_items, a, stream);
     else if (dtype == SPD_BF16)
-        launch<SPD_BF16>(head_dim, modified, tree, n_items, a, stream);
+        launch<SPD_BF16>(head_dim, modified, tree, half, n_items, a, stream);
     else
-        launch<SPD_F16>(head_dim, modified, tree, n_items, a, stream);
+        launch<SPD_F16>(head_dim, modified, tree, half, n_items, a, stream);
 }
 
 }  // namespace spd

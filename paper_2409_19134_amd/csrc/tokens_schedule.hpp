@@ -364,6 +364,7 @@ struct TokTables {
     int64_t pieces[kTokKernels] = {0, 0, 0};
     // The tables serve longer lengths and later queries as well, any of them (growable), or where lengths grow by no more than positions (following).
     bool growable = false, following = false;
+    bool half = false;  // trees: the tiles of many rows are of 64
     int64_t n_items() const
     {
         int64_t n = 0;
@@ -544,6 +545,19 @@ inline void build_tok_tables(const spd_shape *s, const spd_kv_view *v, const std
     for (const TokUserPlan &p : plan)
         if ((int64_t)p.n_tok * G > 16 && (int64_t)p.n_tok * G <= 32)
             few = TokKernel::kFew32;
+    // Trees of many rows go in tiles of 64 where tiles of 128 would be a fifth emptier.  24 users of 900-8000 keys, 32 heads in groups of four of 128, bf16, results in
+    // fp32, us per call in tiles of 128 / 64: 14-16 tokens 136 / 117, 9-32 tokens 141 / 150, 28-32 tokens (results in bf16) 113 / 139.  fp32, six users' 60-64
+    // tokens, 8 heads of 64 55 / 39.
+    if (tree && has_half(s->dtype, s->head_dim)) {
+        int64_t whole = 0, halves = 0;  // rows of all tiles, by the keys they go over
+        for (const TokUserPlan &p : plan)
+            if ((int64_t)p.n_tok * G > 32) {
+                const int64_t rows = (int64_t)p.n_tok * G;
+                whole += (rows + kManyRows - 1) / kManyRows * kManyRows * p.len;
+                halves += (rows + kHalfRows - 1) / kHalfRows * kHalfRows * p.len;
+            }
+        T.half = (double)halves < 0.8 * (double)whole;
+    }
     std::vector<TokTile> tiles[kTokKernels];
     std::vector<TokSteps> spans;
     for (size_t u = 0; u < plan.size(); ++u) {
@@ -571,7 +585,7 @@ inline void build_tok_tables(const spd_shape *s, const spd_kv_view *v, const std
         // would lie in no stretch, so its lengths may only grow with its positions, windows ahead.
         T.following = T.following && k != TokKernel::kMany && p.len > 0 && (!causal || p.q_pos + p.n_tok >= p.len) && !(window && !causal);
         T.growable = T.growable && T.following;
-        const int step = k == TokKernel::kMany ? many_keys(s->dtype) : kFewKeys, cap = tile_rows(k);
+        const int step = k == TokKernel::kMany ? many_keys(s->dtype, T.half) : kFewKeys, cap = k == TokKernel::kMany && T.half ? kHalfRows : tile_rows(k);
         for (int64_t r0 = 0; r0 < rows; r0 += cap) {
             const int64_t r1 = std::min<int64_t>(rows, r0 + cap);
             const TokSpan span = tree ? tile_span(p, causal, window, 0, p.n_tok - 1) : tile_span(p, causal, window, (int)(r0 / G), (int)((r1 - 1) / G));
@@ -586,7 +600,7 @@ inline void build_tok_tables(const spd_shape *s, const spd_kv_view *v, const std
         if (tl.empty())
             continue;
         const bool many = k == (int)TokKernel::kMany;
-        const int step = many ? many_keys(s->dtype) : kFewKeys;
+        const int step = many ? many_keys(s->dtype, T.half) : kFewKeys;
         const int64_t at_once = (int64_t)n_cus * resident((TokKernel)k);
         if (tree && !many) {
             build_few_pieces(v, (TokKernel)k, tl, spans, Hkv, (int64_t)n_cus * tree_resident(s->dtype, s->head_dim, tile_rows((TokKernel)k)), T);

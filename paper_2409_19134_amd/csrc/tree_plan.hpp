@@ -12,9 +12,11 @@ namespace spd {
 struct PlanUser {
     int32_t token, n, first;  // its first token among all, how many, the position of tokens without a parent
 };
-constexpr int kPlanUsers = 256;
+// Users travel with a launch's arguments, which cost the host by their size: few or many.
+constexpr int kPlanUsers = 256, kPlanFew = 16;
+template <int N>
 struct PlanUsers {
-    PlanUser it[kPlanUsers];
+    PlanUser it[N];
 };
 
 struct PlanArgs {
@@ -32,7 +34,8 @@ __device__ __forceinline__ int plan_parent(const PlanArgs &a, const PlanUser &u,
 }
 
 // Up to 64 tokens: one to a lane, sets and jumps in registers.
-__global__ __launch_bounds__(64) void plan_small_kernel(const PlanArgs a, const PlanUsers users)
+template <int N>
+__global__ __launch_bounds__(64) void plan_small_kernel(const PlanArgs a, const PlanUsers<N> users)
 {
     const PlanUser u = users.it[blockIdx.x];
     const int i = threadIdx.x;
@@ -64,8 +67,8 @@ __global__ __launch_bounds__(64) void plan_small_kernel(const PlanArgs a, const 
 // More tokens, up to `MOST` words of sets in all: every word of every set is a thread's, four or sixteen to a thread; the sets wait in LDS in the order in
 // which they are written.
 constexpr int kPlanThreads = 1024;
-template <int MOST>
-__global__ __launch_bounds__(kPlanThreads) void plan_kernel(const PlanArgs a, const PlanUsers users)
+template <int MOST, int N>
+__global__ __launch_bounds__(kPlanThreads) void plan_kernel(const PlanArgs a, const PlanUsers<N> users)
 {
     constexpr int kMine = MOST / kPlanThreads;
     __shared__ uint64_t sets[MOST];
