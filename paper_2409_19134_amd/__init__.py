@@ -5,4 +5,4 @@ from .binding import (Context, KVView, Rope, Score, SpdError, Tree, make_shape, 
                       SPD_ERR_WORKSPACE, SPD_ERR_HIP, SPD_ERR_NOMEM, SPD_F32, SPD_BF16, SPD_F16, SPD_OPT_HEAD_PER_WAVE, SPD_OPT_TARGET_WG_PER_CU,
                       SPD_OPT_NO_SPLIT_MAX, SPD_OPT_CHUNK_MAX, SPD_OPT_SEG_COST, SPD_OPT_HALF_SKEW,
                       SPD_OPT_RESULT_ROWS, SPD_OPT_STEPS_IN_FLIGHT)
-from .step import DecodeStep, TokenStep  # noqa: F401,E402
+from .step import DecodeStep, TokenStep, TreeStep  # noqa: F401,E402

@@ -7,7 +7,7 @@ from __future__ import annotations
 import numpy as np
 import torch
 
-from .binding import Context, KVView, Rope, Score, make_shape
+from .binding import Context, KVView, Rope, Score, Tree, make_shape
 
 
 class DecodeStep:
@@ -174,3 +174,61 @@ class TokenStep:
         c.spd_partial_attn_tokens(self.shape, q, self.prompt, self.n_new, self.score_in, self.a_in, self.lse_in, stream=stream)
         c.spd_lse_merge(self.a_in, self.lse_in, self.a_out, self.lse_out, self.y, self.lse, self.w_in, stream)
         return self.y, self.lse
+
+
+class TreeStep:
+    """Trees of drafted tokens through all layers' caches: what is drafted behind each user's sequence is planned once, appended to and checked in every layer, and
+    of what is accepted the keys and values move together.
+
+    `views` are the layers' caches that take the tokens (alike but for where they lie): their lengths already count the drafted ones, n_new[u] of user u.  With
+    `prompts` (the other owner's views, a layer each) the sequences begin there: the tokens attend to both caches, and the two partials are merged as in
+    Theorem 1.  `rope` (of one axis), and the keywords of Score that concern a sequence (cap, slopes, window, prefix), are the model's.  Holds the result
+    buffers, which are fp32 and the same for all layers.  The views' lengths are read at every call, so a loop may move them on: to the lengths that
+    are kept after `keep`, and by n_new for the next draft."""
+
+    def __init__(self, ctx: Context, dtype, n_q_heads: int, n_kv_heads: int, head_dim: int, scale: float, views, n_new, words: int = None, rope: Rope = None,
+                 prompts=None, device="cuda:0", **score):
+        self.ctx, self.views, self.prompts, self.rope = ctx, list(views), None if prompts is None else list(prompts), rope
+        self.shape = make_shape(dtype, n_q_heads, n_kv_heads, head_dim, scale)
+        self.n_new = np.ascontiguousarray(n_new, dtype=np.int32)
+        assert rope is None or rope.struct.n_axes == 1
+        T, f32 = int(self.n_new.sum()), dict(device=device, dtype=torch.float32)
+        self.tree = Tree(T, max(1, -(-int(self.n_new.max(initial=0)) // 64)) if words is None else words, device=device)
+        self.q = torch.empty((T, n_q_heads, head_dim), device=device, dtype=dtype)
+        self.a_out, self.lse_out = torch.empty((T, n_q_heads, head_dim), **f32), torch.empty((T, n_q_heads), **f32)
+        begin = None if prompts is None else self.prompts[0].lens
+        self.score_out = Score(k_pos=begin, **score)
+        if prompts is not None:
+            assert len(self.prompts) == len(self.views) and all(np.array_equal(p.lens, begin) for p in self.prompts)
+            self.a_in, self.y = (torch.empty((T, n_q_heads, head_dim), **f32) for _ in range(2))
+            self.lse_in, self.lse, self.w_in = (torch.empty((T, n_q_heads), **f32) for _ in range(3))
+            self.score_in = Score(q_pos=np.zeros_like(begin), **score)
+
+    def _first(self):
+        """Each user's position of tokens without a parent: behind what both caches hold."""
+        own = self.views[0].lens - self.n_new
+        return own if self.prompts is None else self.prompts[0].lens + own
+
+    def plan(self, parents: torch.Tensor, stream=None) -> Tree:
+        """A new draft: parents int32 [T], a token's number among its user's drafted tokens, -1 for none.  Once for all layers; returns the Tree (its positions
+        are the tokens')."""
+        return self.ctx.spd_tree_plan(parents, self.n_new, first=self._first(), tree=self.tree, stream=stream)
+
+    def run(self, layer: int, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, stream=None):
+        """Enqueues one layer of the planned draft; returns (attention, its log-sum-exp).  q, k_new, v_new: [T][heads][d] as the projection leaves them."""
+        c, view = self.ctx, self.views[layer]
+        turned = c.spd_append_tokens(self.shape, view, self.n_new, k_new, v_new, self.rope, self.tree.positions if self.rope is not None else None,
+                                     q if self.rope is not None else None, self.q if self.rope is not None else None, stream)
+        q = q if self.rope is None else turned
+        c.spd_partial_attn_tree(self.shape, q, view, self.n_new, self.tree, self.score_out, self.a_out, self.lse_out, stream=stream)
+        if self.prompts is None:
+            return self.a_out, self.lse_out
+        np.copyto(self.score_in.per_user["q_pos"], self._first())
+        c.spd_partial_attn_tree(self.shape, q, self.prompts[layer], self.n_new, self.tree, self.score_in, self.a_in, self.lse_in, stream=stream)
+        c.spd_lse_merge(self.a_in, self.lse_in, self.a_out, self.lse_out, self.y, self.lse, self.w_in, stream)
+        return self.y, self.lse
+
+    def keep(self, keep: torch.Tensor, n_keep: torch.Tensor, stream=None):
+        """The accepted tokens' keys and values move together behind what the caches held before the draft, in all layers: of user u's part of keep (int32 [T])
+        the first n_keep[u] (int32 [users]) numbers.  The lengths are the caller's to shorten."""
+        self.ctx.spd_keep_tokens(self.shape, self.views, self.n_new, keep, n_keep, stream)
