@@ -156,10 +156,10 @@ def _load() -> C.CDLL:
     tree = [shape, vp, i64, view, vp, C.POINTER(spd_tree), score, vp, i32, fp]
     lib.spd_partial_attn_tree.argtypes = [vp, *tree, vp]
     lib.spd_validate_tree.argtypes = tree
-    keep = [shape, view, i32, vp, vp, vp]
+    keep = [shape, vp, i32, vp, vp, vp]
     lib.spd_keep_tokens.argtypes = [vp, *keep, vp]
     lib.spd_validate_keep.argtypes = keep
-    pages = [shape, view, i32, i32, i32, vp, vp]
+    pages = [shape, vp, i32, i32, i32, vp, vp]
     lib.spd_copy_pages.argtypes = [vp, *pages, vp]
     lib.spd_validate_pages.argtypes = pages
     for name in ("spd_rotate", "spd_append_tokens", "spd_partial_attn_tokens", "spd_validate_rotate", "spd_validate_append",
@@ -312,9 +312,9 @@ class Tree:
         self.struct = spd_tree(int(seen.shape[1]), seen.data_ptr(), depth.data_ptr())
 
 
-def _view_array(views):
-    """The structs of several views, side by side."""
-    return (spd_kv_view * max(1, len(views)))(*[v.struct for v in views])
+def _view_array(views) -> bytes:
+    """The structs of several views, side by side (a ctypes array of them takes 2 us to fill)."""
+    return b"".join([v.struct for v in views])
 
 
 def _new_counts(n_new, n_users: int):
@@ -673,12 +673,12 @@ class Context:
         if not views:
             return
         counts, T = _new_counts(n_last, views[0].struct.n_users)
-        for t, n in ((keep, T), (n_keep, counts.shape[0])):
-            assert t.dtype is torch.int32 and t.is_contiguous() and t.shape == (n,)
+        assert keep.dtype is torch.int32 and keep.is_contiguous() and keep.shape == (T,)
+        assert n_keep.dtype is torch.int32 and n_keep.is_contiguous() and n_keep.shape == counts.shape
         here = {self.device}
         for v in views:
             assert v.devices <= here
-        self._here(None, keep, n_keep)
+        assert keep.get_device() == self.device == n_keep.get_device()
         rc = lib.spd_keep_tokens(self.handle, C.byref(shape), _view_array(views), len(views), _address(counts), keep.data_ptr(), n_keep.data_ptr(),
                                  _stream_ptr(stream, self.device))
         self._check(rc, "spd_keep_tokens")

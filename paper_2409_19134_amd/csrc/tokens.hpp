@@ -16,8 +16,7 @@ struct TokUser {
     int32_t q_pos;                // position of its first new token (grows with grow_q)
     int32_t prefix;               // keys below it are seen by every query
     int32_t k_pos;                // position of key 0, for the ranges
-    int32_t next;                 // (in a TreeItem)
-    int32_t pad[3];
+    int32_t pad[4];
 };
 static_assert(sizeof(TokUser) == 64);
 
@@ -31,11 +30,10 @@ struct TokItem {
 };
 static_assert(sizeof(TokItem) == 32);
 
-// The same with its user beside it, for trees: one read brings all that a workgroup needs to ask for keys.  A workgroup takes several, one after the other: the
-// first is the one with its number, and each names the next.
+// The same with its user beside it, for trees: one read brings all that a workgroup needs to ask for keys.
 struct TreeItem {
     TokItem it;
-    TokUser u;  // u.next: the item after this one, 0: none
+    TokUser u;
 };
 static_assert(sizeof(TreeItem) == 96);
 
@@ -81,8 +79,7 @@ struct TokArgs {
     float *part_o;    // [slot][rows of a tile][D]
     float2 *part_lse; // [slot][rows of a tile]: log2 of the sum, and what the final lse adds to it (natural log)
     ScoreArgs score;
-    TreeArgs tree;    // the kernels' tree form
-    int32_t first_piece;    // ... its items are TreeItems, and the launch's first workgroup's is the first_piece-th
+    TreeArgs tree;    // the kernels' tree form, whose items are TreeItems
 };
 
 // A query row's masks and bias (slope: its head's, 0 without).  It sees the keys in [mlo, mlo + mn) and in [plo, plo + pn).

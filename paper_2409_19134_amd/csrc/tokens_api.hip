@@ -428,7 +428,7 @@ int find_or_build(ContextBase *ctx, TokensState *t, const spd_shape *s, const sp
         copy(off_joins[k], T.joins[k]);
         e->off_items[k] = off_items[k];
         e->off_joins[k] = off_joins[k];
-        e->n_items[k] = tree ? T.pieces[k] : (int64_t)T.items[k].size();
+        e->n_items[k] = (int64_t)(tree ? T.tree[k].size() : T.items[k].size());
         e->n_joins[k] = (int64_t)T.joins[k].size();
         e->slots[k] = T.slots[k];
         e->join_rows[k] = e->join_chunks[k] = 0;
@@ -579,8 +579,7 @@ int attend(ContextBase *ctx, const spd_shape *s, const void *q, int64_t q_stride
         a.part_o = t->part + rows[k] * (size_t)s->head_dim;
         a.part_lse = part_lse + rows[k];
         in_parts(e->n_items[k], [&](int64_t first, unsigned n) {
-            a.items = tree ? items : items + first;
-            a.first_piece = (int32_t)first;
+            a.items = tree ? reinterpret_cast<const TokItem *>(reinterpret_cast<const TreeItem *>(items) + first) : items + first;
             if (k == (int)TokKernel::kMany)
                 launch_tokens_many(s->dtype, s->head_dim, modified, tree != nullptr, e->half, n, a, stream);
             else

@@ -103,10 +103,7 @@ __device__ __forceinline__ void few_item(const TokArgs &a, const TokItem &it, co
     __shared__ __attribute__((aligned(16))) float stage[4][16][kPitch];
     __shared__ float stage_ml[2][4][kRows];
 
-    int tid = threadIdx.x;
-    if constexpr (TREE)  // (made anew for every item: what follows from a lane's number has no registers of its own across them)
-        asm volatile("" : "+v"(tid));
-    const int lane = tid & 63, wave = uniform(tid >> 6);
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int r = lane & 15, grp = lane >> 4;
     const int len = u.len + a.grow_len, q_pos0 = u.q_pos + a.grow_q;
     const int k_end = it.k_end + (it.to_len ? a.grow_len : 0);
@@ -393,15 +390,8 @@ template <int DT, int D, bool PAGED, int NT, bool MOD, bool TREE>
 __global__ __launch_bounds__(256, TREE ? tree_resident(DT, D, 16 * NT) : 2) void tokens_few_kernel(const TokArgs a)
 {
     if constexpr (TREE) {
-        int i = a.first_piece + (int)blockIdx.x;
-        do {
-            const TreeItem x = scalar_load(reinterpret_cast<const TreeItem *>(a.items), i);
-            if (x.it.n_rows != 0)  // (else it fills up the launch order)
-                few_item<DT, D, PAGED, NT, MOD, TREE>(a, x.it, x.u);
-            i = x.u.next;
-            if (i != 0)
-                __syncthreads();  // (LDS is written anew)
-        } while (i != 0);
+        const TreeItem x = scalar_load(reinterpret_cast<const TreeItem *>(a.items), blockIdx.x);
+        few_item<DT, D, PAGED, NT, MOD, TREE>(a, x.it, x.u);
     } else {
         const TokItem it = scalar_load(a.items, blockIdx.x);
         const TokUser u = scalar_load(a.users, it.user);

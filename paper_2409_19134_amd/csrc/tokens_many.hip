@@ -582,7 +582,7 @@ __global__ __launch_bounds__(256, 2) void tokens_many_kernel(const TokArgs a)
     __shared__ __attribute__((aligned(16))) char k_lds[2][Tiles<DT, D, FORM>::kBytes], v_lds[2][Tiles<DT, D, FORM>::kBytes];
     const Tiles<DT, D, FORM> lds = {k_lds, v_lds};
     if constexpr (FORM != kChain) {
-        const TreeItem x = scalar_load(reinterpret_cast<const TreeItem *>(a.items), a.first_piece + (int)blockIdx.x);
+        const TreeItem x = scalar_load(reinterpret_cast<const TreeItem *>(a.items), blockIdx.x);
         if (x.it.n_rows == 0)
             return;  // (fills up the launch order)
         many_item<DT, D, EXACT, MOD, FORM>(a, x.it, x.u, lds);

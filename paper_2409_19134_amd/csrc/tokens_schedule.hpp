@@ -4,6 +4,7 @@
 #include <cmath>
 #include <cstdint>
 #include <cstring>
+#include <tuple>
 #include <vector>
 
 #include "host_checks.hpp"
@@ -360,8 +361,7 @@ struct TokTables {
     std::vector<TokItem> items[kTokKernels];  // the launch order
     std::vector<TokJoin> joins[kTokKernels];
     int64_t slots[kTokKernels] = {0, 0, 0};
-    std::vector<TreeItem> tree[kTokKernels];  // trees' items in the place of the others: as many pieces' first ones, then the rest
-    int64_t pieces[kTokKernels] = {0, 0, 0};
+    std::vector<TreeItem> tree[kTokKernels];  // trees' items, in the place of the others
     // The tables serve longer lengths and later queries as well, any of them (growable), or where lengths grow by no more than positions (following).
     bool growable = false, following = false;
     bool half = false;  // trees: the tiles of many rows are of 64
@@ -443,94 +443,6 @@ inline int64_t stretch_steps(const std::vector<TokTile> &tiles, int64_t at_once,
 
 constexpr int kXcds = 8;
 
-// Trees of few rows: the steps of one head's tiles, laid end to end, cut into equal pieces, and every piece one workgroup for each head, side by side in the
-// launch's order: they read the same tokens at the same time.  As many as can run at once.  A workgroup's stretch that begins or ends a tile costs
-// `overhead` steps (its start, its end), and none but a tile's rest is shorter than `least`.
-inline void build_few_pieces(const spd_kv_view *v, TokKernel kernel, const std::vector<TokTile> &tiles, const std::vector<TokSteps> &spans, int n_heads,
-                             int64_t at_once, TokTables &T)
-{
-    const int k = (int)kernel;
-    const int64_t least = 4, overhead = 3;
-    int64_t steps = 0, n_tiles = 0;
-    for (const TokTile &t : tiles)
-        if (t.kv_head == 0) {
-            steps += t.steps;
-            ++n_tiles;
-        }
-    const int64_t line = steps + overhead * n_tiles;
-    const int64_t n = std::max<int64_t>(1, std::min(at_once / n_heads, std::max(steps / least, n_tiles)));
-    auto end_of = [&](int64_t p) { return (line * (p + 1) + n - 1) / n; };
-    struct Part {
-        TokItem it;
-        int64_t piece;
-    };
-    std::vector<Part> parts;  // of head 0
-    int64_t piece = 0, done = 0;  // the piece that is being filled, and the line's length up to here
-    for (const TokTile &t : tiles) {
-        if (t.kv_head != 0)
-            continue;
-        const TokSteps &sp = spans[(size_t)t.first];
-        const int32_t len = v->lens[t.user];
-        const size_t first = parts.size();
-        int32_t s = 0;
-        do {
-            while (piece + 1 < n && end_of(piece) - done < overhead + std::min<int64_t>(least, t.steps - s))
-                ++piece;
-            int64_t take = t.steps - s;
-            if (piece + 1 < n) {
-                const int64_t room = std::max(least, end_of(piece) - done - overhead);
-                if (room < take)
-                    take = take - room < least ? take : room;
-            }
-            TokItem it = {t.user, 0, t.row0, t.n_rows, 0, 0, -1, 0};
-            if (take > 0) {
-                it.k_begin = (int32_t)sp.begin(s, kFewKeys);
-                it.k_end = (int32_t)std::min<int64_t>(sp.begin((int32_t)(s + take - 1), kFewKeys) + kFewKeys, len);
-            }
-            s += (int32_t)take;
-            it.to_len = take > 0 && s == t.steps && it.k_end == len;
-            parts.push_back(Part{it, piece});
-            done += take + (s == t.steps ? overhead : 0);
-        } while (s < t.steps);
-        const int32_t n_parts = (int32_t)(parts.size() - first);
-        if (n_parts > 1) {  // (a whole tile writes its results)
-            for (int32_t j = 0; j < n_parts; ++j)
-                parts[first + (size_t)j].it.slot = (int32_t)(T.slots[k] + j);
-            for (int h = 0; h < n_heads; ++h)
-                T.joins[k].push_back(TokJoin{t.user, h, t.row0, t.n_rows, (int32_t)(T.slots[k] + (int64_t)h * n_parts), n_parts, {0, 0}});
-            for (int32_t j = 0; j < n_parts; ++j)
-                parts[first + (size_t)j].it.to_len |= n_parts << 1;  // (for the other heads' slots, below)
-            T.slots[k] += (int64_t)n_heads * n_parts;
-        }
-    }
-    // Every piece's first item, in the launch's order, then the others, each named by the one before it.
-    int64_t n_pieces = 0;
-    for (size_t i = 0; i < parts.size(); ++i)
-        n_pieces += i == 0 || parts[i].piece != parts[i - 1].piece;
-    T.pieces[k] = n_pieces * n_heads;
-    std::vector<TreeItem> &list = T.tree[k];
-    list.resize(parts.size() * (size_t)n_heads);
-    size_t firsts = 0, others = (size_t)T.pieces[k], at = 0;
-    for (size_t i = 0; i < parts.size(); ++i) {
-        const bool first = i == 0 || parts[i].piece != parts[i - 1].piece;
-        size_t &next = first ? firsts : others;
-        const int32_t n_parts = parts[i].it.to_len >> 1;
-        for (int h = 0; h < n_heads; ++h) {
-            TreeItem &x = list[next + (size_t)h];
-            x.it = parts[i].it;
-            x.it.to_len &= 1;
-            x.it.kv_head = h;
-            if (n_parts)
-                x.it.slot += h * n_parts;
-            x.u = T.users[(size_t)x.it.user];
-            if (!first)
-                list[at + (size_t)h].u.next = (int32_t)(next + (size_t)h);
-        }
-        at = next;
-        next += (size_t)n_heads;
-    }
-}
-
 // tree: a user's tokens lie at any depth, in any order, so every tile's rows may see what any of the user's can.
 inline void build_tok_tables(const spd_shape *s, const spd_kv_view *v, const std::vector<TokUserPlan> &plan, int causal, int window, int n_cus,
                              TokTables &T, bool tree = false)
@@ -601,14 +513,10 @@ inline void build_tok_tables(const spd_shape *s, const spd_kv_view *v, const std
             continue;
         const bool many = k == (int)TokKernel::kMany;
         const int step = many ? many_keys(s->dtype, T.half) : kFewKeys;
-        const int64_t at_once = (int64_t)n_cus * resident((TokKernel)k);
-        if (tree && !many) {
-            build_few_pieces(v, (TokKernel)k, tl, spans, Hkv, (int64_t)n_cus * tree_resident(s->dtype, s->head_dim, tile_rows((TokKernel)k)), T);
-            continue;
-        }
+        const int64_t at_once = (int64_t)n_cus * (tree && !many ? tree_resident(s->dtype, s->head_dim, tile_rows((TokKernel)k)) : resident((TokKernel)k));
         // (a step of many rows is short for its partial's 64 KB; fp32 steps take longer)
-        const double overhead = k == (int)TokKernel::kFew16 ? 2.5 : many && s->dtype != SPD_F32 ? 10.0 : 5.0;
-        const int64_t chunk = stretch_steps(tl, at_once, tree ? 1 : 4, overhead);
+        const double overhead = k == (int)TokKernel::kFew16 && !tree ? 2.5 : many && s->dtype != SPD_F32 ? 10.0 : 5.0;
+        const int64_t chunk = stretch_steps(tl, at_once, tree && many ? 1 : 4, overhead);
         // The longest stretches first.  The many kernel's tiles of one head read the same keys: they go to one XCD (workgroup i
         // runs on XCD i % 8), whose L2 then holds them; heads in order of their work, each to the XCD with least so far.  Where that would
         // leave XCDs idle (their number divides that of the heads badly, and these are few) a head's tiles are dealt out to several.
@@ -672,13 +580,17 @@ inline void build_tok_tables(const spd_shape *s, const spd_kv_view *v, const std
         }
         size_t longest = 0;
         for (auto &x : queue) {
-            std::stable_sort(x.begin(), x.end(), [](const Queued &a, const Queued &b) { return a.steps > b.steps; });
+            // (few rows of a tree: the heads of a stretch side by side; one user's 8 tokens over 6000 keys 17.4 us per call, head by head 20.3)
+            std::stable_sort(x.begin(), x.end(), [&](const Queued &a, const Queued &b) {
+                if (a.steps != b.steps || !tree || many)
+                    return a.steps > b.steps;
+                return std::tie(a.item.user, a.item.row0, a.item.k_begin) < std::tie(b.item.user, b.item.row0, b.item.k_begin);
+            });
             longest = std::max(longest, x.size());
         }
         const TokItem nothing = {0, 0, 0, 0, 0, 0, -1, 0};
         if (tree) {
-            T.pieces[k] = (int64_t)(longest * queue.size());
-            T.tree[k].reserve((size_t)T.pieces[k]);
+            T.tree[k].reserve(longest * queue.size());
             for (size_t i = 0; i < longest; ++i)
                 for (const auto &x : queue)
                     T.tree[k].push_back(i < x.size() ? TreeItem{x[i].item, T.users[(size_t)x[i].item.user]} : TreeItem{nothing, TokUser()});

@@ -1,6 +1,6 @@
 // Host logic of the attention of trees: tables and masks for random users and trees, checked against the masks' definition - every row in one tile, every key
-// that a row sees in exactly one of its tile's stretches and on the walk over it, its bits and masks as they should be, every item in one
-// workgroup's chain with its own user beside it, partial slots given out once, in the order of the keys.
+// that a row sees in exactly one of its tile's stretches and on the walk over it, its bits and masks as they should be, every item with
+// its own user beside it, partial slots given out once, in the order of the keys.
 #include <cstdio>
 #include <cstdlib>
 #include <map>
@@ -84,27 +84,15 @@ int main()
             const int cap = half ? kHalfRows : tile_rows((TokKernel)k), waves = k == (int)TokKernel::kMany ? 1 : 4;
             const std::vector<TreeItem> &list = tables.tree[k];
             REQUIRE(tables.items[k].empty());
-            REQUIRE(tables.pieces[k] <= (int64_t)list.size());
-            REQUIRE(k == (int)TokKernel::kMany || tables.pieces[k] <= std::max(4 * n_cus, H));
-            std::vector<char> reached(list.size(), 0), slots((size_t)tables.slots[k], 0);
+            std::vector<char> slots((size_t)tables.slots[k], 0);
             std::map<std::tuple<int, int, int>, std::vector<TokItem>> tiles;
-            for (int64_t b = 0; b < tables.pieces[k]; ++b) {
-                int64_t i = b;
-                do {
-                    REQUIRE(i >= 0 && i < (int64_t)list.size() && !reached[(size_t)i] && (i == b || i >= tables.pieces[k]));
-                    reached[(size_t)i] = 1;
-                    const TreeItem &x = list[(size_t)i];
-                    if (x.it.n_rows) {
-                        TokUser u = tables.users[(size_t)x.it.user];
-                        u.next = x.u.next;
-                        REQUIRE(std::memcmp(&u, &x.u, sizeof u) == 0 && x.it.n_rows <= cap);
-                        tiles[{x.it.user, x.it.kv_head, x.it.row0}].push_back(x.it);
-                    }
-                    i = x.u.next;
-                } while (i != 0);
+            for (const TreeItem &x : list) {
+                REQUIRE(x.it.n_rows > 0 || k == (int)TokKernel::kMany);  // (the many kernel's launch order is filled up)
+                if (x.it.n_rows == 0)
+                    continue;
+                REQUIRE(std::memcmp(&x.u, &tables.users[(size_t)x.it.user], sizeof x.u) == 0 && x.it.n_rows <= cap);
+                tiles[{x.it.user, x.it.kv_head, x.it.row0}].push_back(x.it);
             }
-            for (char r : reached)
-                REQUIRE(r);
             std::map<std::tuple<int, int, int>, TokJoin> joins;
             for (const TokJoin &j : tables.joins[k])
                 joins[{j.user, j.kv_head, j.row0}] = j;

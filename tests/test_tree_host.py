@@ -218,7 +218,7 @@ def test_what_python_refuses():
 
 
 def test_tables_under_asan_ubsan(tmp_path):
-    """tests/host/tree_schedule_fuzz.cpp: every tile's keys in its stretches once, in order, each stretch in one workgroup's chain of items."""
+    """tests/host/tree_schedule_fuzz.cpp: every tile's keys in its stretches once, in order, and the masks key by key."""
     if not os.path.exists(HIPCC):
         pytest.skip("hipcc not found")
     exe = str(tmp_path / "tree_schedule_fuzz")
