@@ -185,3 +185,53 @@ def test_copied_pages(ctx, dtype, H, d, layout, page, pairs, layers):
                                 o = h * strides[1] + t * strides[0]
                                 want[b, o:o + d] = x[a, o:o + d]
                 assert torch.equal(y.cpu().view(torch.uint8), want.view(torch.uint8))
+
+
+def test_pools_of_more_than_four_gigabytes(ctx):
+    """Pages whose first byte lies beyond 2^32, copied and moved within."""
+    import paper_2409_19134_amd as spd
+    H, d, page, pages = 8, 128, 16, 135000      # 32 KB a page, 4.4 GB a pool
+    shape = spd.make_shape(torch.bfloat16, H, H, d, 1.0)
+    pools = [torch.zeros((pages, page, H, d), dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    last = pages - 1
+    for i, t in enumerate(pools):
+        t[last] = torch.randn((page, H, d), generator=torch.Generator().manual_seed(i)).bfloat16().to(DEV)
+    want = [t[last].clone() for t in pools]
+    table = torch.tensor([[last - 7, last - 3]], dtype=torch.int32, device=DEV)
+    view = spd.KVView([2 * page], H * d, d, k_pool=pools[0], v_pool=pools[1], block_table=table, block_size=page, block_stride=page * H * d)
+    ctx.spd_copy_pages(shape, [view], torch.tensor([[last, 3], [last, last - 3]], dtype=torch.int32, device=DEV))
+    keep = torch.arange(page, 2 * page, dtype=torch.int32, device=DEV).repeat(2)
+    ctx.spd_keep_tokens(shape, [view], [2 * page], keep, torch.tensor([page], dtype=torch.int32, device=DEV))
+    torch.cuda.synchronize()
+    for t, w in zip(pools, want):
+        for at in (3, last - 3, last - 7, last):
+            assert torch.equal(t[at], w)
+        assert not bool(t[last - 1].any()) and not bool(t[4].any())
+
+
+def test_copies_recorded_on_another_stream(ctx):
+    import paper_2409_19134_amd as spd
+    H, d, page = 2, 64, 16
+    shape = spd.make_shape(torch.float16, H, H, d, 1.0)
+    pools = [[torch.randn((12, H, page, d), device=DEV).half() for _ in range(2)] for _ in range(9)]
+    views = [spd.KVView([], d, page * d, k_pool=a, v_pool=b, block_size=page, block_stride=H * page * d) for a, b in pools]
+    pairs, count = torch.zeros((3, 2), dtype=torch.int32, device=DEV), torch.zeros(3, dtype=torch.int32, device=DEV)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    side = torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=side):      # (nothing has to run before it is recorded)
+        ctx.spd_copy_pages(shape, views, pairs, count)
+    for step in range(3):
+        rng = np.random.default_rng(step)
+        p, n = rng.permutation(12)[:6].reshape(3, 2).astype(np.int32), rng.integers(0, page + 1, 3).astype(np.int32)
+        want = [[t.clone() for t in kv] for kv in pools]
+        for kv in want:
+            for t in kv:
+                for (a, b), m in zip(p.tolist(), n.tolist()):
+                    t[b, :, :m] = t[a, :, :m]
+        pairs.copy_(torch.from_numpy(p))
+        count.copy_(torch.from_numpy(n))
+        graph.replay()
+        torch.cuda.synchronize()
+        for kv, w in zip(pools, want):
+            assert all(torch.equal(x, y) for x, y in zip(kv, w))

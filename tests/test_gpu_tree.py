@@ -260,7 +260,7 @@ def test_a_chain_is_the_call_without_a_tree(ctx, dtype, new):
     p.check(*ctx.spd_partial_attn_tokens(p.shape, p.q.to(DEV), p.cache.view, p.new, p.score))
 
 
-@pytest.mark.parametrize("new", [[5, 2], [50]])
+@pytest.mark.parametrize("new", [[5, 2], [14], [50]])
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 def test_what_a_branch_does_not_see_does_not_reach_it(ctx, dtype, new):
     """Infinities and NaN in drafted tokens: in the results of the tokens that see them and in no others'."""
@@ -328,3 +328,35 @@ def test_graphs_streams_and_growing_lengths(ctx):
         tree = spd.Tree.of(torch.from_numpy(p.sets).to(DEV), torch.from_numpy(p.depths).to(DEV))
         out, lse = ctx.spd_partial_attn_tree(p.shape, p.q.to(DEV), view, p.new, tree, spd.Score(window=64))
         p.check(out, lse)
+
+
+def test_another_stream(ctx):
+    """All of it on a stream of its own, behind work of that stream that it has to wait for."""
+    p = Problem((8, 2, 64), "bf16", "paged_hnd16", [9, 14], [200, 3], dict(slopes=True), "f32", seed=12).store()
+    side = torch.cuda.Stream()
+    q, out, lse = p.q.to(DEV), torch.empty((p.T, 8, 64), device=DEV), torch.empty((p.T, 8), device=DEV)
+    parents = [random_parents(np.random.default_rng(3), n, "tree") for n in p.new]
+    given = torch.from_numpy(np.concatenate(parents).astype(np.int32)).to(DEV)
+    late = torch.empty_like(given)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)
+        late.copy_(given)
+        tree = ctx.spd_tree_plan(late, p.new)
+        ctx.spd_partial_attn_tree(p.shape, q, p.cache.view, p.new, tree, p.score, out, lse)
+    side.synchronize()
+    p.see, p.depth = zip(*[branches(x) for x in parents])
+    p.check(out, lse)
+
+
+def test_rows_that_see_nothing(ctx):
+    """Empty sets over an empty past, and windows of one key without the token's own bit: zeros and -inf; the others as ever."""
+    for new in ([3, 5], [60]):
+        p = Problem((4, 1, 64), "f16", "nhd", new, [0], dict(window=1), "f32", seed=14, kind="sets")
+        for u, n in enumerate(new):
+            p.see[u][:] = np.eye(n, dtype=bool)
+            p.see[u][::2] = False
+        p.sets = np.concatenate([pack(x, p.sets.shape[1]) for x in p.see])
+        out, lse = p.store().call(ctx)
+        p.check(out, lse)
+        assert bool(torch.isinf(lse).any()) and bool(torch.isfinite(lse).any())
