@@ -906,13 +906,14 @@ int keep_tokens(ContextBase *ctx, const spd_shape *s, const spd_kv_view *views, 
     a.n_heads = s->n_kv_heads;
     const int row_bytes = s->head_dim * es;
     const int32_t longest = *std::max_element(n_last, n_last + U);
+    // Waves of a stream by the longest list that there may be: a wave takes 4 to 16 tokens at a time.  (A few of many are kept at the end of a check.)
     const int waves = longest <= 64 ? 1 : longest <= 512 ? 4 : 16;
     KeepUsers<kKeepUsers> users;
     KeepLayers<kKeepLayers> layers;
     int failed = SPD_OK;
     auto launch = [&](int n_users, int n_layers) {
         const int64_t streams = (int64_t)n_users * n_layers * 2 * s->n_kv_heads;
-        a.slices = 1;
+        a.slices = 1;  // of a row, down to 64 bytes, where there are not streams enough to fill the device
         while (a.slices * 64 < row_bytes && streams * a.slices * waves < 8 * (int64_t)ctx->n_cus)
             a.slices *= 2;
         a.n_streams = (uint32_t)streams;

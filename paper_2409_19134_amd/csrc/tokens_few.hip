@@ -11,6 +11,10 @@
 // six tokens of 24 users over 900-8000 keys, groups of four, pages of 64, bf16, 459 MB: 85 us, 5.4 TB/s, of which the join is 5; one token of 16 users
 // over 512-4096 keys with a distance bias, pages of 16, 150 MB: 33 us, 4.5 TB/s, the join 4.5: stretches of at most 13 steps, so a start (a table's
 // entry, the page numbers, then the first keys: 3 us one behind the other) for a few us of loads.  One user's token over 1531 keys: 11 us, launches.
+// Trees: as in the kernel for many rows; a step with keys of the tree takes a row's bits and, from memory, its eight keys' depths.  All tiles of a call are of 16 or all of 32
+// rows: one launch.  Held to the registers of as many workgroups as its schedule counts on a unit (24 users' 2-4 tokens over 900-8000 keys, 128 channels, bf16: three take 86 us,
+// two, where three are counted, 98).  40 users' 4-8
+// tokens over 300-3000 keys, 8 KV heads of 64, fp16, 131 MB: 39 us, of which the join is 5; the waves wait for keys, 8 KB of them each, one step at a time.
 #include "partial_mfma.hpp"
 #include "tokens.hpp"
 

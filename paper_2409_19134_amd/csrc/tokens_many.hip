@@ -23,6 +23,16 @@
 // barriers alone need 673.  Tried: the next tile's scores between this tile's weights, 962-988; one V buffer and three waves per SIMD, spills, 1134.
 // fp32: 252 tokens of six users over 4474 earlier ones, 64 heads in groups of eight, 2033 us, 112 TFLOP/s, with a cap 2260; 2048 causal tokens, groups of
 // four, 375 us, 92 (a library product: 154; the matrix units are busy 71 % of a busy unit's time, and tiles of 128 rows compute what the diagonal masks).
+//
+// Trees (the forms kTree and kTreeHalf).  A query's position is its depth's.  Keys in front of the tree go by the same rules as ever; of the tree's own, in the last
+// tiles, a row takes 64 bits of its set at once, shifted to the tile's first key, and their positions (for biases, windows shorter than the tree, ranges) wait in LDS.
+// A workgroup's item brings its user along, and the first tile is asked for before the queries and masks are read: a chain of three dependent reads less
+// where a call is a few steps of latency (one user's 16 tokens over 1531 keys, 8 KV heads of 128, 18.0 us with the join, 12.2 with this and stretches down to one step).
+// Measured, 32 query heads in groups of four of 128 channels, bf16: 24 users' 50-64 tokens over 900-8000 keys 164-171 us (0.61-0.64 PFLOP/s, 478 MB at 2.8-2.9 TB/s; the matrix
+// units are busy 41 % of a busy unit's time and the waves wait 32 % of theirs; with all keys in the L2 156), 28-32 tokens 111-115 (4.1 TB/s); 64 query heads, fp16 with a cap, 8
+// users' 31-48 tokens over 8192-32768 keys 329-350 us.
+// Tried for trees: equal pieces of all tiles' steps, a workgroup taking several tiles and up to four workgroups of an XCD a head's keys side by side: 24 users' 50-64 tokens
+// 168 / 169 without, 28-32 tokens 127 / 112; four tiles of 32 keys in flight 190 / 169; a tile's page numbers read one tile ahead 167 / 164.
 #include "tokens.hpp"
 
 namespace spd {
@@ -79,7 +89,8 @@ template <int DT>
 constexpr float kShift = DT == SPD_F16 ? 7.f : 0.f;
 
 // The kernel's forms.  kTree: for the tokens of a tree.  kTreeHalf: the same for up to 64 rows: two waves share 32 rows, each takes half of every tile's keys, and
-// their sums are joined at the end.  (In the other form two of four waves, and with them two of a unit's four SIMDs, would have no rows.)
+// their sums are joined at the end.  (In the other form two of four waves, and with them two of a unit's four SIMDs, would have no rows: 24 users' 14-16 tokens,
+// fp32 results, 117 us for 136; fp32, six users' 60-64 tokens of 8 heads of 64, 39 for 55.)
 enum { kChain = 0, kTree = 1, kTreeHalf = 2 };
 
 template <int DT, int D, int FORM>
