@@ -75,6 +75,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(const PlanArgs a, co
     constexpr int kMine = MOST / kPlanThreads;
     __shared__ uint64_t sets[MOST];
     __shared__ int16_t jumps[2][64 * SPD_MAX_TREE_WORDS];
+    __shared__ int more[16];  // for every step: whether some token still has a jump (a tree of 2^10 tokens takes eleven steps at most)
     const PlanUser u = users.it[blockIdx.x];
     const int tid = threadIdx.x, W = a.words, n = u.n, n_sets = n * W;  // (n is at most kPlanThreads)
     int mine = tid < n ? plan_parent(a, u, tid) : -1;
@@ -90,8 +91,15 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(const PlanArgs a, co
             sets[e] = token[m] >> 6 == word ? 1ull << (token[m] & 63) : 0ull;
         token[m] = e < n_sets ? token[m] : -1;
     }
-    int now = 0;
-    while (__syncthreads_or(mine >= 0) != 0) {
+    if (tid < 16)
+        more[tid] = 0;
+    __syncthreads();
+    for (int step = 0, now = 0;; ++step, now ^= 1) {
+        if (__builtin_amdgcn_ballot_w64(mine >= 0) != 0 && (tid & 63) == 0)
+            more[step] = 1;
+        __syncthreads();  // (the step before this one is done everywhere, too)
+        if (more[step] == 0)
+            break;
         uint64_t other[kMine];
 #pragma unroll
         for (int m = 0; m < kMine; ++m) {
@@ -105,7 +113,6 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(const PlanArgs a, co
         for (int m = 0; m < kMine; ++m)
             if (other[m])
                 sets[m * kPlanThreads + tid] |= other[m];
-        now ^= 1;
     }
     uint64_t *const out = a.seen + (int64_t)u.token * W;
 #pragma unroll
