@@ -580,11 +580,15 @@ inline void build_tok_tables(const spd_shape *s, const spd_kv_view *v, const std
                 T.slots[k] += n;
             }
         }
+        // Few rows of a tree: the heads of a stretch side by side (one user's 4 tokens over 6000 keys, heads of 64 / 128, us per call: 11.7 / 14.7, head by head 13.3 / 15.2),
+        // but not where long stretches' neighbours would ask for halves of the same 256 bytes at once from several XCDs (24 users' 2-4 tokens over 900-8000 keys, token-major heads of 64,
+        // fp16: 56.8, head by head 49.8).
+        const bool halves = v->head_stride < v->token_stride && s->head_dim * es < 256;
+        const bool side_by_side = tree && !many && !(halves && chunk > 8);
         size_t longest = 0;
         for (auto &x : queue) {
-            // (few rows of a tree: the heads of a stretch side by side; one user's 8 tokens over 6000 keys 17.4 us per call, head by head 20.3)
             std::stable_sort(x.begin(), x.end(), [&](const Queued &a, const Queued &b) {
-                if (a.steps != b.steps || !tree || many)
+                if (a.steps != b.steps || !side_by_side)
                     return a.steps > b.steps;
                 return std::tie(a.item.user, a.item.row0, a.item.k_begin) < std::tie(b.item.user, b.item.row0, b.item.k_begin);
             });
