@@ -4,8 +4,8 @@
 // branch(i) = {i} u branch(parent(i)), by doubling: with jump_k(i) the 2^k-th parent, sets grow as s(i) |= s(jump_k(i)), k = 0, 1, ..., until no
 // token has such a parent: log2 of the depth steps instead of its number.  Sets only ever gain members of the branch, so it does not matter
 // whether a step reads another token's set before or after that one's own step.  The depth is the set's size less one.
-// Measured: one user's 13 tokens 1.4 us (a call 6.2: the host's), 256 users' 100-500 tokens in sets of eight words 10 us, one workgroup to a unit: its chain of about
-// eight barriers with LDS reads between them (a word of the sets to a wave, token after token: 12 us for 128 users).
+// Measured: one user's 13 tokens 1.4 us (a call 6: the host's), 256 users' 100-500 tokens in sets of eight words 8.8 us, one workgroup to a unit: its chain of steps,
+// a barrier each with LDS reads between them (two barriers a step: 10.1; a word of the sets to a wave, token after token: 12 us for 128 users).
 #pragma once
 #include "common.hpp"
 
