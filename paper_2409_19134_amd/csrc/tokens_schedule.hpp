@@ -5,6 +5,7 @@
 #include <cstdint>
 #include <cstring>
 #include <tuple>
+#include <utility>
 #include <vector>
 
 #include "host_checks.hpp"
@@ -215,6 +216,22 @@ inline int validate_layers(const spd_shape *s, const spd_kv_view *views, int32_t
     return n_views > 0 && !views ? SPD_ERR_NULL : SPD_OK;
 }
 
+// Whether a cache is among the layers' twice (one of K and V counts too): the same pool under the same block table, or the same buffer of user u.
+// Its tokens would move twice.
+inline bool cache_twice(const spd_kv_view *views, int32_t n_views, int32_t u)
+{
+    std::pair<const void *, const void *> caches[2 * kMaxLayers];
+    auto end = caches;
+    for (int i = 0; i < n_views; ++i) {
+        const spd_kv_view &v = views[i];
+        const bool paged = v.block_size != 0;
+        *end++ = paged ? std::make_pair(v.k_pool, (const void *)v.block_table) : std::make_pair(v.k_ptrs_dev ? (const void *)v.k_ptrs_dev : v.k_ptrs[u], (const void *)nullptr);
+        *end++ = paged ? std::make_pair(v.v_pool, (const void *)v.block_table) : std::make_pair(v.k_ptrs_dev ? (const void *)v.v_ptrs_dev : v.v_ptrs[u], (const void *)nullptr);
+    }
+    std::sort(caches, end);
+    return std::adjacent_find(caches, end) != end;
+}
+
 inline int validate_keep(const spd_shape *s, const spd_kv_view *views, int32_t n_views, const int32_t *n_last, const int32_t *keep, const int32_t *n_keep)
 {
     int rc = validate_layers(s, views, n_views);
@@ -239,6 +256,8 @@ inline int validate_keep(const spd_shape *s, const spd_kv_view *views, int32_t n
         return rc;
     if (!keep || !n_keep)
         return SPD_ERR_NULL;
+    if (cache_twice(views, n_views, (int)(std::find_if(n_last, n_last + views[0].n_users, [](int32_t n) { return n > 0; }) - n_last)))
+        return SPD_ERR_SHAPE;
     return (reinterpret_cast<uintptr_t>(keep) | reinterpret_cast<uintptr_t>(n_keep)) & 3u ? SPD_ERR_ALIGN : SPD_OK;
 }
 

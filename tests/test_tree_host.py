@@ -1,6 +1,7 @@
 """The calls for trees of drafted tokens and for moves within caches without a GPU: what they refuse, what the Python side refuses before the library is
 asked, and their tables."""
 import ctypes as C
+import itertools
 import math
 import os
 import subprocess
@@ -15,6 +16,7 @@ from paper_2409_19134_amd import binding as b
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 P = 0x10000      # an address that is never followed
+_caches = itertools.count(1)      # (no two views of one cache unless a test says so)
 S, L, N, A = spd.SPD_ERR_SHAPE, spd.SPD_ERR_LEN, spd.SPD_ERR_NULL, spd.SPD_ERR_ALIGN
 
 
@@ -56,15 +58,16 @@ class View:
 
     def __init__(self, lens=(20, 30), page=0, **kw):
         self.lens = np.array(lens, np.int32)
-        self.ptrs = (C.c_void_p * max(1, len(lens)))(*[P] * max(1, len(lens)))
+        k, v = self.caches = [next(_caches) * P for _ in "kv"]
+        self.ptrs = [(C.c_void_p * max(1, len(lens)))(*[x] * max(1, len(lens))) for x in (k, v)]
         st = spd.spd_kv_view()
         st.n_users, st.lens = len(lens), self.lens.ctypes.data_as(C.POINTER(C.c_int32))
         st.token_stride, st.head_stride = 64, 64 * 64
         if page:
-            st.k_pool = st.v_pool = st.block_table = P
+            st.k_pool, st.v_pool, st.block_table = k, v, P
             st.block_size, st.max_blocks, st.block_stride = page, 100, 2 * 64 * page
         else:
-            st.k_ptrs = st.v_ptrs = C.cast(self.ptrs, C.POINTER(C.c_void_p))
+            st.k_ptrs, st.v_ptrs = (C.cast(x, C.POINTER(C.c_void_p)) for x in self.ptrs)
         for k, v in kw.items():
             setattr(st, k, v)
         self.struct = st
@@ -106,8 +109,15 @@ def test_refusals_of_kept_tokens():
     assert _keep([View(), View(lens=(20, 29))]) == S and _keep([View(), View(lens=(20, 30, 1))]) == S and _keep([View(), View(page=16)]) == S
     assert _keep([View(), View(token_stride=72)]) == S and _keep([View(), View(head_stride=128)]) == S and _keep([View(page=16), View(page=32)]) == S
     assert _keep([View(page=16), View(page=16, block_stride=4096)]) == S
-    with_dev = View(k_ptrs_dev=P, v_ptrs_dev=P)
-    assert _keep([with_dev, with_dev]) == 0 and _keep([View(), with_dev]) == S
+    with_dev, more = View(k_ptrs_dev=P, v_ptrs_dev=2 * P), View(k_ptrs_dev=3 * P, v_ptrs_dev=4 * P)
+    assert _keep([with_dev, more]) == 0 and _keep([View(), with_dev]) == S
+    # a cache twice
+    view, paged = View(), View(page=16)
+    assert _keep([with_dev, more, with_dev]) == S and _keep([View(k_ptrs_dev=P, v_ptrs_dev=P)]) == S
+    assert _keep([view, View(), view]) == S and _keep([View(k_ptrs=view.struct.v_ptrs), view]) == S and _keep([view, view], n_last=(0, 0)) == 0
+    assert _keep([paged, paged]) == S and _keep([View(page=16, v_pool=paged.caches[0]), paged]) == S and _keep([paged, View(page=16, k_pool=paged.caches[0])]) == S
+    assert _keep([paged, View(page=16, k_pool=paged.caches[0], v_pool=paged.caches[1], block_table=2 * P)]) == 0
+    assert _keep([View(page=16) for _ in range(1024)]) == 0 and _keep([paged] + [View(page=16) for _ in range(1022)] + [paged]) == S
     a, c = (np.array(x, np.int64) for x in ([64, 128], [64, 64]))
     strided = [View(head_strides=x.ctypes.data_as(C.POINTER(C.c_int64))) for x in (a, a, c)]
     assert _keep(strided[:2]) == 0 and _keep(strided) == S and _keep([strided[0], View()]) == S
