@@ -499,7 +499,7 @@ int spd_partial_attn_tree(spd_ctx *ctx, const spd_shape *shape, const void *q, i
  * all the views.  After a check: n_last = the drafted tokens, keep = the accepted branch.  For a cache that is to hold less: n_last =
  * lens, keep = the tokens that stay.  The caller's lengths are its own to shorten.
  *   views    HOST [n_views], 0 .. 1024: the layers' caches, with the same lengths, strides and kind of storage; no cache twice, nor one of
- *            both K and V (SPD_ERR_SHAPE; pools may be shared by views with block tables of their own)
+ *            both K and V (SPD_ERR_SHAPE; pools may be shared by views with block tables of their own, which need not be equally wide)
  *   n_last   HOST [n_users], 0 .. lens[u]; T = their sum, T * Hq at most 2^31 - 1
  *   keep     DEVICE int32 [T], of user u's n_last[u] entries the first n_keep[u]: any with i <= keep[t0 + i] < n_last[u], in any order, the
  *            same one more than once if need be.  An entry that is not in that range leaves its place as it is.

@@ -23,8 +23,11 @@ struct KeepUsers {
 };
 struct KeepLayer {
     char *kv[2];              // paged: the pools; else arrays of the users' buffers, on the device
-    const int32_t *table;     // paged
+    const int32_t *table;     // paged: [users][max_blocks], a width of its own for every layer
+    int32_t max_blocks;
 };
+// A user's row of a layer's block table.
+__host__ __device__ __forceinline__ const int32_t *keep_row(const KeepLayer &l, int user) { return l.table + (int64_t)user * l.max_blocks; }
 constexpr int kKeepLayers = 32, kKeepFewLayers = 8;
 template <int N>
 struct KeepLayers {
@@ -34,7 +37,7 @@ struct KeepLayers {
 struct KeepArgs {
     const int32_t *keep, *n_keep;
     int64_t token_stride, block_stride;  // bytes
-    int32_t max_blocks, page_shift;
+    int32_t page_shift;
     int32_t n_heads, n_layers, slices;
     uint32_t first, n_streams;           // the launch's first stream's number, and how many there are
 };
@@ -76,7 +79,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void keep_kernel(con
     global_i32 *table = nullptr, *const keep = (global_i32 *)(a.keep + u.token);
     if constexpr (PAGED) {
         base = (global_char *)layer.kv[kv] + lane_off;
-        table = (global_i32 *)(layer.table + (int64_t)u.user * a.max_blocks);
+        table = (global_i32 *)keep_row(layer, u.user);
     } else {
         base = (global_char *)reinterpret_cast<char *const *>(layer.kv[kv])[u.user] + lane_off;
     }

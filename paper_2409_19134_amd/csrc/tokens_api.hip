@@ -901,7 +901,6 @@ int keep_tokens(ContextBase *ctx, const spd_shape *s, const spd_kv_view *views, 
     a.n_keep = n_keep;
     a.token_stride = v.token_stride * es;
     a.block_stride = paged ? v.block_stride * es : 0;
-    a.max_blocks = paged ? v.max_blocks : 0;
     a.page_shift = paged ? page_shift(v.block_size) : 0;
     a.n_heads = s->n_kv_heads;
     const int row_bytes = s->head_dim * es;
@@ -965,6 +964,7 @@ int keep_tokens(ContextBase *ctx, const spd_shape *s, const spd_kv_view *views, 
                 const spd_kv_view &l = views[i + j];
                 KeepLayer &x = layers.it[j];
                 x.table = paged ? l.block_table : nullptr;
+                x.max_blocks = paged ? l.max_blocks : 0;
                 if (paged) {
                     x.kv[0] = static_cast<char *>(const_cast<void *>(l.k_pool));
                     x.kv[1] = static_cast<char *>(const_cast<void *>(l.v_pool));
