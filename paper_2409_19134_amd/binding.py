@@ -182,9 +182,22 @@ def make_shape(dtype, n_q_heads: int, n_kv_heads: int, head_dim: int, scale: flo
     return spd_shape(int(dtype), int(n_q_heads), int(n_kv_heads), int(head_dim), float(scale))
 
 
-def _pool_pages(pool: torch.Tensor, block_stride: int) -> int:
-    """Pages of a pool: its first dimension, where that counts pages, else as many as lie in it end to end."""
-    return int(pool.shape[0]) if pool.dim() > 1 and pool.stride(0) == block_stride else pool.numel() // max(1, block_stride)
+def _pool_pages(pool: torch.Tensor, st: spd_kv_view, element: int, n_heads: int, head_dim: int) -> int:
+    """Pages of a pool that lie in its tensor whole, each head's last token too (strides in elements of `element` bytes).  Where heads or tokens lie farther apart than
+    pages, as many as fit between two of them; where the tensor's first dimension counts pages, no more than those."""
+    if st.block_stride <= 0:
+        return 1      # (which the library refuses)
+    if not pool.numel():
+        return 0
+    page = (n_heads - 1) * st.head_stride + (st.block_size - 1) * st.token_stride + head_dim
+    span = (1 + sum((n - 1) * x for n, x in zip(pool.shape, pool.stride()))) * pool.element_size() // element
+    pages = max(0, (span - page) // st.block_stride + 1)
+    for n, stride in ((n_heads, st.head_stride), (st.block_size, st.token_stride)):
+        if n > 1 and stride > st.block_stride:
+            pages = min(pages, stride // st.block_stride)
+    if pool.dim() > 1 and pool.stride(0) * pool.element_size() == st.block_stride * element:
+        pages = min(pages, int(pool.shape[0]))
+    return pages
 
 
 class KVView:
@@ -194,9 +207,11 @@ class KVView:
                  v: Optional[Sequence[torch.Tensor]] = None, k_pool: Optional[torch.Tensor] = None,
                  v_pool: Optional[torch.Tensor] = None, block_table: Optional[torch.Tensor] = None,
                  block_size: int = 0, block_stride: int = 0, max_blocks: Optional[int] = None,
-                 head_strides=None, device_pointer_tables: bool = False):
+                 head_strides=None, device_pointer_tables: bool = False, n_pages: Optional[int] = None):
         """device_pointer_tables (contiguous mode): also hand the per-user pointers over in device arrays, which makes
-        the split schedule independent of the buffers' addresses (views of different layers then share one)."""
+        the split schedule independent of the buffers' addresses (views of different layers then share one).
+        n_pages (paged mode, for spd_copy_pages): how many pages the pools have, at most what the storage behind the tensors holds; None: as many as lie in
+        both tensors (`pages`)."""
         self.lens = np.ascontiguousarray(lens, dtype=np.int32)
         n = int(self.lens.shape[0])
         self._keep = (k, v, k_pool, v_pool, block_table)
@@ -223,11 +238,27 @@ class KVView:
                 st.k_ptrs_dev, st.v_ptrs_dev = self._kp_dev.data_ptr(), self._vp_dev.data_ptr()
         else:
             st.k_pool, st.v_pool = k_pool.data_ptr(), v_pool.data_ptr()
-            self.n_pages = min(_pool_pages(t, int(block_stride)) for t in (k_pool, v_pool))
+            self._given, self._counted = n_pages, None
             if block_table is not None:      # (copies of pages go without one)
                 st.block_table = block_table.data_ptr()
                 st.max_blocks = int(block_table.shape[1] if max_blocks is None else max_blocks)
         self.struct = st
+        if block_size:
+            self.n_pages = n_pages if n_pages is not None else min(_pool_pages(t, st, t.element_size(), 1, 1) for t in (k_pool, v_pool))
+
+    def pages(self, shape: spd_shape) -> int:
+        """Pages of the pools for heads of this shape (n_pages: before it is known)."""
+        of = shape.dtype, shape.n_kv_heads, shape.head_dim
+        if self._counted is None or self._counted[0] != of:
+            element, st, pools = 4 if shape.dtype == SPD_F32 else 2, self.struct, self._keep[2:4]
+            if self._given is None:
+                n = min(_pool_pages(t, st, element, *of[1:]) for t in pools)
+            else:
+                n = self._given
+                last = (n - 1) * st.block_stride + (of[1] - 1) * st.head_stride + (st.block_size - 1) * st.token_stride + of[2]
+                assert n >= 0 and all(n == 0 or last * element <= t.untyped_storage().nbytes() - t.storage_offset() * t.element_size() for t in pools)
+            self._counted = of, n
+        return self._counted[1]
 
     @classmethod
     def from_side(cls, side, device_pointer_tables: bool = False) -> "KVView":
@@ -685,7 +716,7 @@ class Context:
 
     def spd_copy_pages(self, shape, views: Sequence[KVView], pairs: torch.Tensor, n_tokens: Optional[torch.Tensor] = None, stream=None):
         """In all the (paged) views' pools, pages copied: pairs int32 [n, 2], from page and to page; n_tokens (int32 [n]): only so many first tokens
-        of each.  A page that is copied to may be in no other pair."""
+        of each.  A page that is copied to may be in no other pair.  Pairs with a number that no page of the pools has (KVView.pages) are left out."""
         if not views:
             return
         assert pairs.dtype is torch.int32 and pairs.is_contiguous() and pairs.dim() == 2 and pairs.shape[1] == 2
@@ -693,7 +724,7 @@ class Context:
         here = {self.device}
         for v in views:
             assert v.struct.block_size and v.devices <= here
-        n_pages = min([v.n_pages for v in views])
+        n_pages = min([v.pages(shape) for v in views])
         self._here(None, pairs, n_tokens)
         rc = lib.spd_copy_pages(self.handle, C.byref(shape), _view_array(views), len(views), n_pages, pairs.shape[0],
                                 pairs.data_ptr(), None if n_tokens is None else n_tokens.data_ptr(), _stream_ptr(stream, self.device))

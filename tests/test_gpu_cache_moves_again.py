@@ -39,3 +39,33 @@ def test_kept_tokens_with_tables_of_other_widths(ctx, n_last, past, layout, dtyp
         torch.cuda.synchronize()
         for c, x in zip(caches, want):
             assert all(torch.equal(a, b) for a, b in zip(c.bits(), x.bits()))
+
+
+@pytest.mark.parametrize("dtype,H,d", [(torch.bfloat16, 4, 64), (torch.float32, 3, 128)])
+@pytest.mark.parametrize("layout", ["k_v_side_by_side", "heads_outermost", "heads_outermost_flat"])
+def test_pages_of_pools_in_other_orders(ctx, layout, dtype, H, d):  # noqa: F811
+    """The last page is copied, and a number that no page has is left out, whatever the storage would hold there."""
+    import paper_2409_19134_amd as spd
+    page, pages = 16, 8
+    shape = spd.make_shape(dtype, H, H, d, 1.0)
+    gen = torch.Generator().manual_seed(9)
+    if layout == "k_v_side_by_side":
+        flat = torch.randn(pages * 2 * H * page * d, generator=gen).to(dtype).to("cuda:0")
+        whole = [flat]
+        pools, strides = (flat, flat[H * page * d:]), (d, page * d, 2 * H * page * d)
+        by_page = [flat.view(pages, 2, H, page, d)[:, i] for i in range(2)]
+    else:
+        whole = [torch.randn((H, pages, page, d), generator=gen).to(dtype).to("cuda:0") for _ in range(2)]
+        pools, strides = [t.view(-1) if layout.endswith("flat") else t for t in whole], (d, pages * page * d, page * d)
+        by_page = [t.transpose(0, 1) for t in whole]
+    view = spd.KVView([], strides[0], strides[1], k_pool=pools[0], v_pool=pools[1], block_size=page, block_stride=strides[2])
+    assert view.pages(shape) == pages
+    want = [t.clone() for t in by_page]
+    given = [[7, 0], [2, 6], [8, 1], [3, 9], [4, 31], [1 << 20, 5]]
+    for t in want:
+        t[0], t[6] = t[7].clone(), t[2].clone()
+    ctx.spd_copy_pages(shape, [view], torch.tensor(given, dtype=torch.int32, device="cuda:0"))
+    torch.cuda.synchronize()
+    for t, w in zip(by_page, want):
+        assert torch.equal(t, w)
+    assert all(bool(torch.isfinite(t).all()) for t in whole)
