@@ -498,8 +498,10 @@ int spd_partial_attn_tree(spd_ctx *ctx, const spd_shape *shape, const void *q, i
  * b + keep[t0 + i] held before the call, for i < n_keep[u] (t0: the sum of the n_last in front of u's), in K and V, in all heads of
  * all the views.  After a check: n_last = the drafted tokens, keep = the accepted branch.  For a cache that is to hold less: n_last =
  * lens, keep = the tokens that stay.  The caller's lengths are its own to shorten.
- *   views    HOST [n_views], 0 .. 1024: the layers' caches, with the same lengths, strides and kind of storage; no cache twice, nor one of
- *            both K and V (SPD_ERR_SHAPE; pools may be shared by views with block tables of their own, which need not be equally wide)
+ *   views    HOST [n_views], 0 .. 1024: the layers' caches, with the same lengths, strides and kind of storage.  No cache twice, nor one of
+ *            both K and V: refused (SPD_ERR_SHAPE) where two have the same pool and block table, the same array on the device, or the same buffer
+ *            of a user with tokens (by the host's pointers).  Pools may be shared by views with block tables of their own, which need not be
+ *            equally wide; that those name other pages is the caller's to see to
  *   n_last   HOST [n_users], 0 .. lens[u]; T = their sum, T * Hq at most 2^31 - 1
  *   keep     DEVICE int32 [T], of user u's n_last[u] entries the first n_keep[u]: any with i <= keep[t0 + i] < n_last[u], in any order, the
  *            same one more than once if need be.  An entry that is not in that range leaves its place as it is.

@@ -849,7 +849,8 @@ void with_row_bytes(int bytes, F &&f)
 int keep_tokens(ContextBase *ctx, const spd_shape *s, const spd_kv_view *views, int32_t n_views, const int32_t *n_last, const int32_t *keep,
                 const int32_t *n_keep, hipStream_t stream)
 {
-    int rc = validate_keep(s, views, n_views, n_last, keep, n_keep);
+    const bool remembered = n_views > 0 && views && views[0].block_size == 0 && !views[0].k_ptrs_dev;  // (by all that buffers_twice looks at)
+    int rc = validate_keep(s, views, n_views, n_last, keep, n_keep, !remembered);
     if (rc != SPD_OK || n_views == 0)
         return rc;
     const spd_kv_view &v = views[0];
@@ -864,7 +865,7 @@ int keep_tokens(ContextBase *ctx, const spd_shape *s, const spd_kv_view *views, 
     const bool paged = v.block_size != 0;
     // Buffers without pointer arrays on the device: the pointers of all layers, remembered by themselves ([layer][K, V][user]).
     const char *uploaded = nullptr;
-    if (!paged && !v.k_ptrs_dev) {
+    if (remembered) {
         TokensState *t = state_of(ctx);
         const bool in_graph = recording(stream);
         const size_t n = (size_t)n_views * 2 * (size_t)U;
@@ -880,6 +881,8 @@ int keep_tokens(ContextBase *ctx, const spd_shape *s, const spd_kv_view *views, 
         TokEntry *e = find(t->entries[2], t->key, hash);
         if (e) {
             use_entry(t, *e, stream, in_graph);
+        } else if (buffers_twice(views, n_views, n_last)) {
+            return SPD_ERR_SHAPE;
         } else if (in_graph) {
             return cannot_record(ctx);
         } else {

@@ -216,23 +216,51 @@ inline int validate_layers(const spd_shape *s, const spd_kv_view *views, int32_t
     return n_views > 0 && !views ? SPD_ERR_NULL : SPD_OK;
 }
 
-// Whether a cache is among the layers' twice (one of K and V counts too): the same pool under the same block table, or the same buffer of user u.
-// Its tokens would move twice.
-inline bool cache_twice(const spd_kv_view *views, int32_t n_views, int32_t u)
+// Whether a cache is among the layers' twice (one of K and V counts too): its tokens would move twice.  Pages: the same pool under the same block table (that
+// tables which lie apart name other pages is for the caller to see to).  Buffers: the same array of pointers on the device, or the same buffer of a user whose tokens
+// move (buffers_twice: the arrays on the device are copies of the host's).
+inline bool tables_twice(const spd_kv_view *views, int32_t n_views)
 {
     std::pair<const void *, const void *> caches[2 * kMaxLayers];
     auto end = caches;
     for (int i = 0; i < n_views; ++i) {
         const spd_kv_view &v = views[i];
         const bool paged = v.block_size != 0;
-        *end++ = paged ? std::make_pair(v.k_pool, (const void *)v.block_table) : std::make_pair(v.k_ptrs_dev ? (const void *)v.k_ptrs_dev : v.k_ptrs[u], (const void *)nullptr);
-        *end++ = paged ? std::make_pair(v.v_pool, (const void *)v.block_table) : std::make_pair(v.k_ptrs_dev ? (const void *)v.v_ptrs_dev : v.v_ptrs[u], (const void *)nullptr);
+        *end++ = paged ? std::make_pair(v.k_pool, (const void *)v.block_table) : std::make_pair((const void *)v.k_ptrs_dev, (const void *)nullptr);
+        *end++ = paged ? std::make_pair(v.v_pool, (const void *)v.block_table) : std::make_pair((const void *)v.v_ptrs_dev, (const void *)nullptr);
     }
     std::sort(caches, end);
     return std::adjacent_find(caches, end) != end;
 }
+inline bool buffers_twice(const spd_kv_view *views, int32_t n_views, const int32_t *n_last)
+{
+    // A set of addresses, emptied for the next user by the user's number beside each.
+    constexpr int kMost = 4 * kMaxLayers;
+    const void *place[kMost];
+    int32_t owner[kMost];
+    int bits = 3;
+    while ((1 << bits) < 4 * n_views)
+        ++bits;
+    std::fill(owner, owner + (1 << bits), -1);
+    for (int32_t u = 0; u < views[0].n_users; ++u) {
+        if (n_last[u] == 0)
+            continue;
+        for (int i = 0; i < n_views; ++i)
+            for (const void *p : {views[i].k_ptrs[u], views[i].v_ptrs[u]}) {
+                uint32_t at = (uint32_t)((uint64_t)reinterpret_cast<uintptr_t>(p) * 0x9e3779b97f4a7c15ull >> (64 - bits));
+                for (; owner[at] == u; at = (at + 1) & ((1u << bits) - 1))  // (half of the places are free)
+                    if (place[at] == p)
+                        return true;
+                owner[at] = u;
+                place[at] = p;
+            }
+    }
+    return false;
+}
 
-inline int validate_keep(const spd_shape *s, const spd_kv_view *views, int32_t n_views, const int32_t *n_last, const int32_t *keep, const int32_t *n_keep)
+// buffers: with the check for buffers that are given twice, which a call that remembers them makes once.
+inline int validate_keep(const spd_shape *s, const spd_kv_view *views, int32_t n_views, const int32_t *n_last, const int32_t *keep, const int32_t *n_keep,
+                         bool buffers = true)
 {
     int rc = validate_layers(s, views, n_views);
     for (int i = 0; rc == SPD_OK && i < n_views; ++i) {
@@ -256,7 +284,8 @@ inline int validate_keep(const spd_shape *s, const spd_kv_view *views, int32_t n
         return rc;
     if (!keep || !n_keep)
         return SPD_ERR_NULL;
-    if (cache_twice(views, n_views, (int)(std::find_if(n_last, n_last + views[0].n_users, [](int32_t n) { return n > 0; }) - n_last)))
+    const bool paged = views[0].block_size != 0;
+    if (((paged || views[0].k_ptrs_dev) && tables_twice(views, n_views)) || (!paged && buffers && buffers_twice(views, n_views, n_last)))
         return SPD_ERR_SHAPE;
     return (reinterpret_cast<uintptr_t>(keep) | reinterpret_cast<uintptr_t>(n_keep)) & 3u ? SPD_ERR_ALIGN : SPD_OK;
 }

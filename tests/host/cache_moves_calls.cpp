@@ -90,14 +90,65 @@ static void tables()
     }
 }
 
+// Buffers that are given twice, through the call that remembers tables of pointers: refused each time, whatever was remembered before and after.
+static void twice()
+{
+    SYM(spd_keep_tokens);
+    for (const bool dev : {false, true}) {
+        spd_ctx *ctx = make();
+        constexpr int U = 5, kViews = 3;
+        const spd_shape s = {SPD_BF16, 8, 2, 64, 0.1f};
+        const std::vector<int32_t> lens(U, 40), n_last = {4, 0, 9, 40, 1};
+        std::vector<const void *> k[kViews], v[kViews];
+        std::vector<spd_kv_view> views(kViews);
+        for (int i = 0; i < kViews; ++i) {
+            for (int u = 0; u < U; ++u) {
+                k[i].push_back(static_cast<char *>(kNowhere) + ((int64_t)(2 * i) * U + u) * (1 << 20));
+                v[i].push_back(static_cast<char *>(kNowhere) + ((int64_t)(2 * i + 1) * U + u) * (1 << 20));
+            }
+            spd_kv_view &x = views[(size_t)i];
+            x = {};
+            x.n_users = U;
+            x.lens = lens.data();
+            x.token_stride = 64;
+            x.head_stride = 64 * 64;
+            x.k_ptrs = k[i].data();
+            x.v_ptrs = v[i].data();
+            if (dev) {
+                x.k_ptrs_dev = k[i].data();
+                x.v_ptrs_dev = v[i].data();
+            }
+        }
+        auto call = [&] {
+            return spd_keep_tokens_(ctx, &s, views.data(), kViews, n_last.data(), static_cast<const int32_t *>(kNowhere), static_cast<const int32_t *>(kNowhere), nullptr);
+        };
+        for (int round = 0; round < 3; ++round)
+            for (int u = 0; u < U; ++u) {
+                const void *const own = v[2][(size_t)u];
+                const size_t before = launches.size();
+                const int uploaded = uploads;
+                v[2][(size_t)u] = k[1][(size_t)u];
+                const int rc = call();
+                if (rc != (n_last[(size_t)u] ? SPD_ERR_SHAPE : SPD_OK) || (rc != SPD_OK && (launches.size() != before || uploads != uploaded)))
+                    FAIL("twice: user %d of round %d: %d", u, round, rc);
+                v[2][(size_t)u] = own;
+                if (call() != SPD_OK)
+                    FAIL("twice: the call without it fails");
+            }
+        drop(ctx);
+    }
+}
+
 int main(int argc, char **argv)
 {
     const std::string what = argc > 2 ? argv[2] : "";
     lib = argc > 2 ? dlopen(argv[1], RTLD_NOW) : nullptr;
     if (!lib)
-        FAIL("cache_moves_calls <library> tables");
+        FAIL("cache_moves_calls <library> tables | twice");
     if (what == "tables")
         tables();
+    else if (what == "twice")
+        twice();
     else
         FAIL("no such part");
     std::printf("ok\n");

@@ -29,3 +29,8 @@ def _run(program, *args):
 def test_kept_tokens_of_block_tables_of_their_own_widths(program):
     """Layers whose block tables are not equally wide: each user's pages come from its own row of its layer's table."""
     _run(program, "tables")
+
+
+def test_buffers_given_twice(program):
+    """Refused before anything is launched, also by the call that remembers the pointers of calls before."""
+    _run(program, "twice")
