@@ -200,6 +200,11 @@ def _pool_pages(pool: torch.Tensor, st: spd_kv_view, element: int, n_heads: int,
     return pages
 
 
+def _heads_of(shape: spd_shape) -> int:
+    """Type, KV heads and their channels in one number."""
+    return (shape.n_kv_heads << 40) + (shape.head_dim << 8) + shape.dtype
+
+
 class KVView:
     """Marshalled spd_kv_view; keeps the host arrays (and the tensors they point into) alive."""
 
@@ -238,27 +243,28 @@ class KVView:
                 st.k_ptrs_dev, st.v_ptrs_dev = self._kp_dev.data_ptr(), self._vp_dev.data_ptr()
         else:
             st.k_pool, st.v_pool = k_pool.data_ptr(), v_pool.data_ptr()
-            self._given, self._counted = n_pages, None
+            self._given = n_pages
             if block_table is not None:      # (copies of pages go without one)
                 st.block_table = block_table.data_ptr()
                 st.max_blocks = int(block_table.shape[1] if max_blocks is None else max_blocks)
-        self.struct = st
-        if block_size:
+        self.struct, self.paged, self._counted_for = st, block_size != 0, None
+        if self.paged:
             self.n_pages = n_pages if n_pages is not None else min(_pool_pages(t, st, t.element_size(), 1, 1) for t in (k_pool, v_pool))
 
     def pages(self, shape: spd_shape) -> int:
         """Pages of the pools for heads of this shape (n_pages: before it is known)."""
-        of = shape.dtype, shape.n_kv_heads, shape.head_dim
-        if self._counted is None or self._counted[0] != of:
+        of = _heads_of(shape)
+        if self._counted_for != of:
+            assert self.paged
             element, st, pools = 4 if shape.dtype == SPD_F32 else 2, self.struct, self._keep[2:4]
-            if self._given is None:
-                n = min(_pool_pages(t, st, element, *of[1:]) for t in pools)
+            H, d, n = shape.n_kv_heads, shape.head_dim, self._given
+            if n is None:
+                n = min(_pool_pages(t, st, element, H, d) for t in pools)
             else:
-                n = self._given
-                last = (n - 1) * st.block_stride + (of[1] - 1) * st.head_stride + (st.block_size - 1) * st.token_stride + of[2]
+                last = (n - 1) * st.block_stride + (H - 1) * st.head_stride + (st.block_size - 1) * st.token_stride + d
                 assert n >= 0 and all(n == 0 or last * element <= t.untyped_storage().nbytes() - t.storage_offset() * t.element_size() for t in pools)
-            self._counted = of, n
-        return self._counted[1]
+            self._counted_for, self._counted = of, n
+        return self._counted
 
     @classmethod
     def from_side(cls, side, device_pointer_tables: bool = False) -> "KVView":
@@ -721,10 +727,12 @@ class Context:
             return
         assert pairs.dtype is torch.int32 and pairs.is_contiguous() and pairs.dim() == 2 and pairs.shape[1] == 2
         assert n_tokens is None or (n_tokens.dtype is torch.int32 and n_tokens.is_contiguous() and n_tokens.shape == (pairs.shape[0],))
-        here = {self.device}
+        here, of, n_pages = {self.device}, _heads_of(shape), (1 << 31) - 1
         for v in views:
-            assert v.struct.block_size and v.devices <= here
-        n_pages = min([v.pages(shape) for v in views])
+            assert v.devices <= here
+            n = v._counted if v._counted_for == of else v.pages(shape)
+            if n < n_pages:
+                n_pages = n
         self._here(None, pairs, n_tokens)
         rc = lib.spd_copy_pages(self.handle, C.byref(shape), _view_array(views), len(views), n_pages, pairs.shape[0],
                                 pairs.data_ptr(), None if n_tokens is None else n_tokens.data_ptr(), _stream_ptr(stream, self.device))
