@@ -680,10 +680,13 @@ class Context:
 
     def spd_tree_plan(self, parents: torch.Tensor, n_new, first=None, words: Optional[int] = None, tree: Optional[Tree] = None, stream=None) -> Tree:
         """The Tree of drafted tokens from their parents (int32 [T]: a number among the user's own drafted tokens, -1: none), n_new[u] of user u;
-        with first (a host sequence: the position of each user's tokens without a parent) its positions too.  tree: one to write into."""
+        with first (a host sequence: the position of each user's tokens without a parent) its positions too.  tree: one to write into (without first, what
+        it has of positions stays as it is; a new one has none)."""
         counts, T = _new_counts(n_new, len(n_new))
         if tree is None:
             tree = Tree(T, max(1, -(-int(counts.max(initial=0)) // 64)) if words is None else words, device=parents.device)
+            if first is None:
+                tree.positions = None
         assert words is None or tree.struct.n_words == words
         assert parents.dtype is torch.int32 and parents.is_contiguous() and parents.shape == (T,) and tree.seen.shape[0] == T
         begin = None
