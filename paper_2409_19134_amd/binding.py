@@ -248,11 +248,15 @@ class KVView:
                 st.block_table = block_table.data_ptr()
                 st.max_blocks = int(block_table.shape[1] if max_blocks is None else max_blocks)
         self.struct, self.paged, self._counted_for = st, block_size != 0, None
-        if self.paged:
-            self.n_pages = n_pages if n_pages is not None else min(_pool_pages(t, st, t.element_size(), 1, 1) for t in (k_pool, v_pool))
+
+    @property
+    def n_pages(self) -> int:
+        """Pages of the pools before the heads' shape is known."""
+        assert self.paged
+        return self._given if self._given is not None else min(_pool_pages(t, self.struct, t.element_size(), 1, 1) for t in self._keep[2:4])
 
     def pages(self, shape: spd_shape) -> int:
-        """Pages of the pools for heads of this shape (n_pages: before it is known)."""
+        """Pages of the pools for heads of this shape."""
         of = _heads_of(shape)
         if self._counted_for != of:
             assert self.paged
