@@ -487,7 +487,9 @@ int spd_tree_plan(spd_ctx *ctx, int32_t n_users, const int32_t *n_new, const int
  * q_pos the view holds none of them (another owner's cache) and the sets say nothing.  Positions: user u's token t has q_pos[u] + depth[t],
  * or, without q_pos, k_pos[u] + lens[u] - n_new[u] + depth[t], as a query and as a key; distances, windows and ranges go by these.  The score's prefix
  * is one of the keys in front of the tree; causal makes no difference among the tree's own keys.
- * Everything else is as there: results, their roundings, recording and scratch memory (it is the same entry point's).
+ * Everything else is as there: results, their roundings, recording and scratch memory (it is the same entry point's).  Lengths that move on by another
+ * number for every user have a table built and uploaded: once for views that differ in pools, block tables or k_ptrs_dev / v_ptrs_dev alone, for every
+ * layer where contiguous views come without those arrays.
  */
 int spd_partial_attn_tree(spd_ctx *ctx, const spd_shape *shape, const void *q, int64_t q_token_stride, const spd_kv_view *view,
                           const int32_t *n_new, const spd_tree *tree, const spd_score *score, void *out, int32_t out_dtype, float *lse,

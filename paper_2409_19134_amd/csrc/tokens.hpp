@@ -469,7 +469,7 @@ __attribute__((visibility("hidden"))) void launch_tokens_many(int dtype, int hea
 constexpr int kManyRows = 128;  // rows of a tile of the many kernel
 constexpr int kHalfRows = 64;   // ... of its form (of trees) in which two waves share 32 rows
 __host__ __device__ constexpr int many_keys(int dtype, bool half = false) { return dtype == SPD_F32 && !half ? 32 : 64; }  // keys of its steps
-// Where there is such a form (fp32 heads of 128 have no room for steps of 64 keys in LDS).
+// Where there is such a form.  (Steps of 64 keys of fp32 heads of 128 take 128 KB of LDS: one workgroup to a unit instead of two.  Not tried.)
 __host__ __device__ constexpr bool has_half(int dtype, int head_dim) { return dtype != SPD_F32 || head_dim == 64; }
 // Workgroups of the few kernel's tree form that fit on a compute unit, by its rows.
 __host__ __device__ constexpr int tree_resident(int dtype, int head_dim, int rows)

@@ -28,9 +28,9 @@
 // tiles, a row takes 64 bits of its set at once, shifted to the tile's first key, and their positions (for biases, windows shorter than the tree, ranges) wait in LDS.
 // A workgroup's item brings its user along, and the first tile is asked for before the queries and masks are read: a chain of three dependent reads less
 // where a call is a few steps of latency (one user's 16 tokens over 1531 keys, 8 KV heads of 128, 18.0 us with the join, 12.2 with this and stretches down to one step).
-// Measured, 32 query heads in groups of four of 128 channels, bf16: 24 users' 50-64 tokens over 900-8000 keys 164-171 us (0.61-0.64 PFLOP/s, 478 MB at 2.8-2.9 TB/s; the matrix
+// Measured, 32 query heads in groups of four of 128 channels, bf16: 24 users' 50-64 tokens over 900-8000 keys 167-171 us (0.61-0.62 PFLOP/s, 478 MB at 2.8-2.9 TB/s; the matrix
 // units are busy 41 % of a busy unit's time and the waves wait 32 % of theirs; with all keys in the L2 156), 28-32 tokens 111-115 (4.1 TB/s); 64 query heads, fp16 with a cap, 8
-// users' 31-48 tokens over 8192-32768 keys 329-350 us.
+// users' 31-48 tokens over 8192-32768 keys 332-347 us.
 // Tried for trees: equal pieces of all tiles' steps, a workgroup taking several tiles and up to four workgroups of an XCD a head's keys side by side: 24 users' 50-64 tokens
 // 168 / 169 without, 28-32 tokens 127 / 112; four tiles of 32 keys in flight 190 / 169; a tile's page numbers read one tile ahead 167 / 164.
 #include "tokens.hpp"

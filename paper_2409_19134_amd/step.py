@@ -184,7 +184,8 @@ class TreeStep:
     `prompts` (the other owner's views, a layer each) the sequences begin there: the tokens attend to both caches, and the two partials are merged as in
     Theorem 1.  `rope` (of one axis), and the keywords of Score that concern a sequence (cap, slopes, window, prefix), are the model's.  Holds the result
     buffers, which are fp32 and the same for all layers.  The views' lengths are read at every call, so a loop may move them on: to the lengths that
-    are kept after `keep`, and by n_new for the next draft."""
+    are kept after `keep`, and by n_new for the next draft.  (Such lengths have a table built: once a step for paged views, and for contiguous ones made with
+    device_pointer_tables, else for every layer.)"""
 
     def __init__(self, ctx: Context, dtype, n_q_heads: int, n_kv_heads: int, head_dim: int, scale: float, views, n_new, words: int = None, rope: Rope = None,
                  prompts=None, device="cuda:0", **score):
